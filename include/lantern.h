@@ -24,6 +24,14 @@
  *   lantern_verify_trees_greedy   the tree step under greedy decoding
  *   lantern_verify_trees_sequential   the tree step with siblings verified one
  *                      after the other against the residual of those before
+ * and what the target model does around a tree step, on its paged cache of
+ * keys and values:
+ *   lantern_rotate_axes     rotary positions with several axes, for the tokens
+ *                      of images
+ *   lantern_attend_trees    attention of the drafted tokens to the cache and to
+ *                      their branch of the tree (single tokens: a tree of no
+ *                      candidates)
+ *   lantern_append_cache    the rows that were kept, or a prompt's, into the cache
  *
  * Naming.  The paper writes p for the drafter and q for the target model.
  * Other texts use the letters the other way round, so this header uses
@@ -60,7 +68,9 @@ extern "C" {
 
 typedef enum {
     LANTERN_F32 = 0,  /* IEEE binary32                       */
-    LANTERN_BF16 = 1  /* bfloat16 (upper 16 bits of binary32) */
+    LANTERN_BF16 = 1, /* bfloat16 (upper 16 bits of binary32) */
+    LANTERN_E4M3 = 2  /* 8 bits: sign, 4 of exponent, 3 of mantissa, largest 448, no
+                         infinity; of caches alone, with scales beside them     */
 } lantern_dtype;
 
 typedef enum {
@@ -496,6 +506,163 @@ int lantern_verify_trees_sequential(const void* target_logits, const void* draft
                                     const int32_t* knn, int k, int divergence, float delta, const float* uniforms,
                                     int32_t* out_len, int32_t* out_path, int32_t* out_next, void* workspace,
                                     size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Rotary positions with several axes (row and column of an image token, its
+ * frame or its place in the text).  The pairs of a head are dealt to the axes in
+ * runs; pair j of axis a is turned by phi = positions[row, a] * freqs[j]:
+ *   y1 = x1 cos phi - x2 sin phi,  y2 = x1 sin phi + x2 cos phi
+ * With P pairs in all, pair j is (x[2j], x[2j+1]) when interleaved is not zero
+ * and (x[j], x[j+P]) when it is; the elements from 2P on are not turned.
+ *   positions  device, [rows, axes] int32, negative ones too
+ *   freqs      device, [P] float32, radians to a step of the position
+ *   axes       1 .. LANTERN_MAX_AXES;  pairs[a] >= 0, their sum P from 1 to D/2
+ * Angle, cosine and sine are evaluated in fp64, cosine and sine rounded to
+ * binary32, the products and their sum in binary32 (each rounded on its own).
+ */
+#define LANTERN_MAX_AXES 4
+#define LANTERN_MAX_HEAD 1024
+typedef struct {
+    const int32_t* positions;
+    const float* freqs;
+    int axes;
+    int pairs[LANTERN_MAX_AXES];
+    int interleaved;
+} lantern_rotation;
+
+/*
+ * Paged cache of the keys and values of one layer, device memory of the caller.
+ * Token t of a sequence is slot t % page_tokens of the page that the sequence's
+ * row of a page table names for t / page_tokens.
+ *   k  [pages, heads, page_tokens, D]
+ *   v  [pages, heads, D, page_tokens]: the tokens of one element in a row, as the
+ *      matrix instructions of lantern_attend_trees take them
+ *   k_scale, v_scale  [pages, heads] float32, positive: under LANTERN_E4M3 a
+ *      value is its code times the scale of its page and head (else not read)
+ *   dtype        LANTERN_BF16 or LANTERN_E4M3
+ *   page_tokens  16, 32, 64 or 128;  D  32, 64, 96 or 128;  heads <= 65535
+ * k and v are 16-byte aligned.  The struct itself lies in host memory and is
+ * read during the call.
+ */
+typedef struct {
+    void* k;
+    void* v;
+    float* k_scale;
+    float* v_scale;
+    lantern_dtype dtype;
+    int pages;
+    int heads;
+    int page_tokens;
+    int D;
+} lantern_cache;
+
+/*
+ * Turns the queries and keys of N tokens by their positions, in one launch.
+ *   q, out_q  device, N rows of q_heads heads of D elements, dtype (F32, BF16);
+ *             *_strides: host, elements from a row to the next and from a head
+ *             to the next (a head's elements are dense)
+ *   k, out_k  the same with k_heads; NULL with k_heads = 0
+ *   inverse   not zero: turned back (-phi).  The map is orthogonal, so that is
+ *             also its gradient: with the outputs' gradients for q and k the
+ *             outputs are the inputs' gradients.
+ * An output may be its input (same address and strides); other overlaps are
+ * undefined.  Errors: E_DTYPE, E_SHAPE (N < 0, q_heads < 1, k_heads < 0,
+ * D < 2, D > LANTERN_MAX_HEAD, the rotation's limits), E_NULL, E_DEVICE.  N = 0 does nothing.
+ */
+int lantern_rotate_axes(const void* q, const int64_t* q_strides, int q_heads, const void* k, const int64_t* k_strides,
+                        int k_heads, lantern_dtype dtype, int N, int D, const lantern_rotation* rotation, int inverse,
+                        void* out_q, const int64_t* out_q_strides, void* out_k, const int64_t* out_k_strides,
+                        void* hip_stream);
+
+/*
+ * Appends rows of keys and values to the cache of B sequences.
+ *   table     device, [B, table_width] int32: the pages of each sequence in order;
+ *             entries behind the last page that is reached are not read
+ *   lengths   device, [B] int32: tokens that the cache holds of each sequence; a
+ *             negative one marks a place without a sequence: nothing is done there
+ *   k, v      device, B sequences of T rows of the cache's heads of D elements, dtype
+ *             (F32, BF16); *_strides: host, elements from a sequence, row and head
+ *             to the next
+ *   rotation  NULL, or the rotation of the keys, its positions [B * T, axes]: a
+ *             key is turned in binary32 and rounded once, to the cache's type
+ *   path, count  which rows.  path NULL: the first count[b] (count NULL: all T).
+ *             path [B, T-1] int32 with count [B], as lantern_verify_trees leaves
+ *             them in out_path and out_len: row 0 (the token before the
+ *             candidates), then the rows 1 + path[b, j] for j < count[b], in that order
+ *   out_lengths [B] int32, not the array `lengths`: the new lengths.  -2: the
+ *             sequence was left as it is, because count is negative or beyond the
+ *             rows, a path entry is outside [0, T-1), the table is too narrow, or
+ *             an entry of it that is needed outside [0, pages).
+ * E4M3 pages: the scale of a page and head is the smallest power of two s >=
+ * 2^-126 with |x| <= 448 s for the finite values that go in; a page that
+ * holds earlier tokens of the sequence keeps the larger of its scale and that,
+ * and when the scale grows their codes are rounded to it.  Codes are rounded to
+ * nearest, ties to even; a value that is not finite is stored as NaN (bf16
+ * pages keep infinities).  Slots behind the new length keep what they hold.
+ * Pages written here must belong to one sequence of the call alone, and the
+ * rows must not overlap the cache.
+ * Errors: E_DTYPE, E_SHAPE (limits above; B < 0, T < 1, table_width < 1 or more
+ * tokens than INT_MAX, path without T > 1, B * touched pages beyond INT_MAX,
+ * out_lengths == lengths), E_NULL (also path without count), E_DEVICE.  B = 0 does nothing.
+ */
+int lantern_append_cache(const lantern_cache* cache, const int32_t* table, int table_width, const int32_t* lengths, int B,
+                         int T, const void* k, const int64_t* k_strides, const void* v, const int64_t* v_strides,
+                         lantern_dtype dtype, const lantern_rotation* rotation, const int32_t* path, const int32_t* count,
+                         int32_t* out_lengths, void* hip_stream);
+
+/*
+ * Attention of B draft trees of M candidates over the cache.  A sequence has
+ * M + 1 rows: row 0 is the token before the candidates (the last one that was
+ * kept; its key and value are not in the cache yet), row 1 + i is candidate i.
+ * A row sees the cached tokens of its sequence, and of the sequence's own rows
+ * itself, its ancestors and row 0.  M = 0 is decoding token by token; with
+ * parent NULL every row follows the one before it (part of a prompt).
+ *   out = sum_j softmax_j(scale * q . k_j) v_j  over what the row sees
+ *   q        device, B sequences of M + 1 rows of q_heads heads of D elements,
+ *            dtype (F32, BF16); query head i belongs to key head
+ *            i / (q_heads / cache->heads)
+ *   k, v     device, the rows' own keys (turned, if the cache's are) and values, of
+ *            the cache's heads; *_strides: host, elements from a sequence, row and
+ *            head to the next
+ *   parent   device, [B*M] int32 as in lantern_verify_trees, or NULL.  A candidate
+ *            whose parent is outside [-1, i), and what follows such a one, is not
+ *            there: its row of the output is zero and no row sees it.
+ *   table, table_width, lengths  as in lantern_append_cache; lengths may be 0, and
+ *            all rows of a place without a sequence (negative) are zero
+ *   scale    of the scores, finite and >= 0
+ *   out      device, [B, M+1, q_heads, D] dense, dtype
+ *   workspace  device memory, 256-byte aligned, of at least
+ *            lantern_attend_trees_workspace_bytes; owned by the caller, contents
+ *            unspecified afterwards, must not be shared by calls that may
+ *            overlap.  May be NULL where that says 0.
+ * Slots behind a sequence's length and rows that a row does not see have no
+ * influence, whatever they hold.  A row that sees nothing with a weight is zero.
+ * A page that is needed and outside [0, pages), or a table too narrow for a length,
+ * makes all of the sequence's rows NaN that are there.  A row that sees a value of the
+ * sequence's own that is not finite has NaN in that element.
+ * Scores, maxima, sums and outputs are held in binary32.  With F32 the products are
+ * formed in binary32 throughout; with BF16 the weights (times the values' scale)
+ * are rounded to bfloat16 for the second product, half a step of 2^-8 each.
+ * Errors: E_DTYPE, E_SHAPE (B < 0, M < 0, M > LANTERN_MAX_TREE, q_heads not a
+ * positive multiple of the cache's heads, table_width < 1 or more tokens than INT_MAX, the
+ * cache's limits, scale not finite or negative, more workgroups or rows than INT_MAX),
+ * E_NULL, E_WORKSPACE, E_DEVICE.  B = 0 does nothing.
+ */
+#define LANTERN_MAX_TREE 255
+size_t lantern_attend_trees_workspace_bytes(lantern_dtype dtype, int B, int M, int q_heads, const lantern_cache* cache,
+                                            int table_width);
+
+int lantern_attend_trees(const void* q, const int64_t* q_strides, const void* k, const int64_t* k_strides, const void* v,
+                         const int64_t* v_strides, lantern_dtype dtype, int B, int M, int q_heads, const int32_t* parent,
+                         const lantern_cache* cache, const int32_t* table, int table_width, const int32_t* lengths,
+                         float scale, void* out, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * lantern_prepare for the three calls above: loads their kernels for this type and
+ * cache and raises their LDS limits on the current device.
+ * Errors: E_DTYPE, E_SHAPE, E_NULL (no cache; its pointers are not looked at), E_DEVICE.
+ */
+int lantern_prepare_cache(lantern_dtype dtype, const lantern_cache* cache);
 
 /*
  * Measurement aid, not part of the method: reads the first bytes / 65536 whole

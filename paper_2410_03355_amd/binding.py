@@ -17,12 +17,13 @@ import importlib.machinery
 import importlib.util
 import os
 import warnings
+from typing import NamedTuple, Optional
 
 import torch
 
 from .build import LIB_PATH, MARSHAL_PATH, marshal_built_for
 
-F32, BF16 = 0, 1
+F32, BF16, E4M3 = 0, 1, 2
 METRIC_L2, METRIC_COSINE = 0, 1
 MAX_VOCAB = 1 << 19
 
@@ -36,9 +37,25 @@ EXPORTS = (
     "lantern_build_random", "lantern_decide_rows", "lantern_resample_selected", "lantern_verify_trees",
     "lantern_verify_trees_greedy", "lantern_verify_trees_sequential_workspace_bytes",
     "lantern_verify_trees_sequential", "lantern_probe_stream_read", "lantern_prepare", "lantern_build_knn_static",
-    "lantern_status_string",
+    "lantern_rotate_axes", "lantern_append_cache", "lantern_attend_trees_workspace_bytes", "lantern_attend_trees",
+    "lantern_prepare_cache", "lantern_status_string",
     "lantern_version",
 )
+
+MAX_AXES = 4
+MAX_TREE = 255
+
+
+class _Rotation(ctypes.Structure):
+    _fields_ = [("positions", ctypes.c_void_p), ("freqs", ctypes.c_void_p), ("axes", ctypes.c_int),
+                ("pairs", ctypes.c_int * MAX_AXES), ("interleaved", ctypes.c_int)]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("dtype", ctypes.c_int), ("pages", ctypes.c_int), ("heads", ctypes.c_int), ("page_tokens", ctypes.c_int),
+                ("D", ctypes.c_int)]
+
 
 _lib = None
 _marshal = None
@@ -109,6 +126,20 @@ def load() -> ctypes.CDLL:
     lib.lantern_build_knn_static.restype = i32
     lib.lantern_prepare.argtypes = [i32, i32, i32]
     lib.lantern_prepare.restype = i32
+    strides = ctypes.POINTER(i64)
+    lib.lantern_rotate_axes.argtypes = [vp, strides, i32, vp, strides, i32, i32, i32, i32, ctypes.POINTER(_Rotation), i32,
+                                        vp, strides, vp, strides, vp]
+    lib.lantern_rotate_axes.restype = i32
+    lib.lantern_append_cache.argtypes = [ctypes.POINTER(_Cache), vp, i32, vp, i32, i32, vp, strides, vp, strides, i32,
+                                         ctypes.POINTER(_Rotation), vp, vp, vp, vp]
+    lib.lantern_append_cache.restype = i32
+    lib.lantern_attend_trees_workspace_bytes.argtypes = [i32, i32, i32, i32, ctypes.POINTER(_Cache), i32]
+    lib.lantern_attend_trees_workspace_bytes.restype = sz
+    lib.lantern_attend_trees.argtypes = [vp, strides, vp, strides, vp, strides, i32, i32, i32, i32, vp, ctypes.POINTER(_Cache),
+                                         vp, i32, vp, f32, vp, vp, sz, vp]
+    lib.lantern_attend_trees.restype = i32
+    lib.lantern_prepare_cache.argtypes = [i32, ctypes.POINTER(_Cache)]
+    lib.lantern_prepare_cache.restype = i32
     lib.lantern_status_string.argtypes = [i32]
     lib.lantern_status_string.restype = ctypes.c_char_p
     lib.lantern_version.argtypes = []
@@ -682,3 +713,199 @@ def verify_trees_greedy(target_logits, row_index, parent, M: int, draft_tokens, 
     if rc != OK:
         raise LanternError(rc, "lantern_verify_trees_greedy")
     return acc, tok, n, path, nxt
+
+
+class Cache(NamedTuple):
+    """Paged cache of one layer's keys and values (lantern_cache): k [pages, heads, page_tokens, D] and
+    v [pages, heads, D, page_tokens], bfloat16, or float8_e4m3fn with k_scale and v_scale [pages, heads] float32.
+    The calls take any tuple of these four."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+
+
+def make_cache(pages: int, heads: int, page_tokens: int, D: int, dtype=torch.float8_e4m3fn, device="cuda") -> Cache:
+    """An empty cache (zeros, scales of one)."""
+    if dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+        raise TypeError("a cache is bfloat16 or float8_e4m3fn")
+    if page_tokens not in (16, 32, 64, 128) or D not in (32, 64, 96, 128) or pages < 1 or heads < 1:
+        raise ValueError("page_tokens must be 16, 32, 64 or 128, D 32, 64, 96 or 128, pages and heads positive")
+    k = torch.zeros((pages, heads, page_tokens, D), dtype=dtype, device=device)
+    v = torch.zeros((pages, heads, D, page_tokens), dtype=dtype, device=device)
+    if dtype == torch.bfloat16:
+        return Cache(k, v)
+    return Cache(k, v, torch.ones((pages, heads), device=device), torch.ones((pages, heads), device=device))
+
+
+def _need_here(stream, *tensors):
+    """Device tensors, all on the current device: the kernels are launched there."""
+    _need_cuda(*tensors)
+    here = torch.cuda.current_device()
+    if any(t is not None and t.device.index != here for t in tensors) or (stream is not None and stream.device.index != here):
+        raise ValueError("all tensors and the stream must belong to the current device")
+
+
+def _made_for(stream, *tensors):
+    """Tensors allocated here for work on a stream of the caller's: their memory is not given away before that is done."""
+    if stream is not None:
+        for t in tensors:
+            t.record_stream(stream)
+
+
+def _strides(*values):
+    return (ctypes.c_int64 * len(values))(*values)
+
+
+def _cache_args(cache):
+    """(lantern_cache, its tensors) of a cache's tensors."""
+    k, v, k_scale, v_scale = cache
+    if k.dim() != 4 or v.dim() != 4 or not (k.is_contiguous() and v.is_contiguous()):
+        raise ValueError("the cache must be two contiguous tensors, [pages, heads, page_tokens, D] and [pages, heads, D, page_tokens]")
+    pages, heads, page_tokens, D = k.shape
+    if tuple(v.shape) != (pages, heads, D, page_tokens) or k.dtype != v.dtype:
+        raise ValueError("the cache's keys and values must have the same sizes and dtype")
+    scales = ()
+    if k.dtype == torch.float8_e4m3fn:
+        scales = (k_scale, v_scale)
+        for s in scales:
+            if s is None or s.dtype != torch.float32 or tuple(s.shape) != (pages, heads) or not s.is_contiguous():
+                raise ValueError("an 8-bit cache needs k_scale and v_scale, contiguous float32 [pages, heads]")
+    elif k.dtype != torch.bfloat16:
+        raise TypeError("a cache is bfloat16 or float8_e4m3fn")
+    c = _Cache(k.data_ptr(), v.data_ptr(), scales[0].data_ptr() if scales else None, scales[1].data_ptr() if scales else None,
+               E4M3 if scales else BF16, pages, heads, page_tokens, D)
+    return c, (k, v, *scales)
+
+
+def _table_args(table, lengths, B):
+    if table.dtype != torch.int32 or lengths.dtype != torch.int32:
+        raise TypeError("table and lengths must be int32")
+    if table.dim() != 2 or table.shape[0] != B or table.shape[1] < 1 or lengths.numel() != B or \
+            not (table.is_contiguous() and lengths.is_contiguous()):
+        raise ValueError("table must be contiguous [B, pages of a sequence], lengths contiguous [B]")
+
+
+def _rotation_args(positions, freqs, sections, interleaved, rows: int):
+    sections = tuple(int(n) for n in sections)
+    if positions.dtype != torch.int32 or freqs.dtype != torch.float32:
+        raise TypeError("positions must be int32, freqs float32")
+    if not 1 <= len(sections) <= MAX_AXES or positions.numel() != rows * len(sections) or freqs.numel() != sum(sections) or \
+            not (positions.is_contiguous() and freqs.is_contiguous()):
+        raise ValueError("positions must be contiguous with one entry per row and axis, freqs with one per pair of the sections")
+    return _Rotation(positions.data_ptr(), freqs.data_ptr(), len(sections), (ctypes.c_int * MAX_AXES)(*sections), int(bool(interleaved)))
+
+
+def rotate_axes(q, k, positions, freqs, sections, interleaved: bool = False, inverse: bool = False, out=None, stream=None):
+    """lantern_rotate_axes: q [N, heads, D] and k [N, heads, D] (or None) turned by positions [N, axes]; sections: pairs of
+    each axis, freqs [their sum].  Returns (q, k) turned, new tensors or those of `out` (a pair, which may be q and k
+    themselves).  inverse turns back, which is the gradient: it takes the outputs' gradients to the inputs'."""
+    lib = load()
+    ts = [t for t in (q, k) if t is not None]
+    for t in ts:
+        if t.dim() != 3 or t.shape[0] != q.shape[0] or t.shape[2] != q.shape[2] or t.dtype != q.dtype or (t.shape[2] > 1 and t.stride(2) != 1):
+            raise ValueError("q and k must be [N, heads, D] of the same N, D and dtype, with dense heads")
+    _need_here(stream, *ts, positions, freqs)
+    N, _, D = q.shape
+    code = _dtype_code(q)
+    rot = _rotation_args(positions, freqs, sections, interleaved, N)
+    if out is None:
+        outs = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in ts]
+        _made_for(stream, *outs)
+    else:
+        outs = [t for t in out if t is not None]
+        if len(outs) != len(ts) or any(o.shape != t.shape or o.dtype != t.dtype or (D > 1 and o.stride(2) != 1) for o, t in zip(outs, ts)):
+            raise ValueError("out must hold tensors like q and k, with dense heads")
+        _need_here(stream, *outs)
+    has_k = k is not None
+    rc = lib.lantern_rotate_axes(q.data_ptr(), _strides(*q.stride()[:2]), q.shape[1], k.data_ptr() if has_k else None,
+                                 _strides(*k.stride()[:2]) if has_k else None, k.shape[1] if has_k else 0, code, N, D,
+                                 ctypes.byref(rot), int(bool(inverse)), outs[0].data_ptr(), _strides(*outs[0].stride()[:2]),
+                                 outs[1].data_ptr() if has_k else None, _strides(*outs[1].stride()[:2]) if has_k else None,
+                                 _stream_ptr(stream))
+    if rc != OK:
+        raise LanternError(rc, "lantern_rotate_axes")
+    return outs[0], outs[1] if has_k else None
+
+
+def _rows_of_cache(cache: _Cache, k, v):
+    if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.shape[2] != cache.heads or k.shape[3] != cache.D or \
+            k.stride(3) != 1 or v.stride(3) != 1:
+        raise ValueError("k and v must be [B, rows, heads, D] of the cache's heads and D, of one dtype, with dense heads")
+
+
+def append_cache(cache, table, lengths, k, v, positions=None, freqs=None, sections=None, interleaved: bool = False,
+                 path=None, count=None, stream=None):
+    """lantern_append_cache: rows of k and v [B, T, heads, D] into the pages of table [B, width] from lengths [B] on, the keys
+    turned by positions [B, T, axes] if given.  Which rows: path [B, T-1] and count [B] as verify_trees returns them (row 0,
+    then the accepted candidates), or the first count [B], or all.  Returns the new lengths int32[B] (-2: left as it was)."""
+    lib = load()
+    c, parts = _cache_args(cache)
+    _rows_of_cache(c, k, v)
+    B, T = k.shape[:2]
+    _table_args(table, lengths, B)
+    rot = None
+    if positions is not None:
+        if freqs is None or sections is None:
+            raise ValueError("positions come with freqs and sections")
+        rot = _rotation_args(positions, freqs, sections, interleaved, B * T)
+    for t, n in ((path, B * (T - 1)), (count, B)):
+        if t is not None and (t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous()):
+            raise ValueError("path must be a contiguous int32 [B, T-1], count a contiguous int32 [B]")
+    if path is not None and count is None:
+        raise ValueError("path comes with count")
+    _need_here(stream, *parts, table, lengths, k, v, positions, freqs, path, count)
+    out = torch.empty(B, dtype=torch.int32, device=k.device)
+    _made_for(stream, out)
+    rc = lib.lantern_append_cache(ctypes.byref(c), table.data_ptr(), table.shape[1], lengths.data_ptr(), B, T, k.data_ptr(),
+                                  _strides(*k.stride()[:3]), v.data_ptr(), _strides(*v.stride()[:3]), _dtype_code(k),
+                                  None if rot is None else ctypes.byref(rot), None if path is None else path.data_ptr(),
+                                  None if count is None else count.data_ptr(), out.data_ptr(), _stream_ptr(stream))
+    if rc != OK:
+        raise LanternError(rc, "lantern_append_cache")
+    return out
+
+
+def attend_trees_workspace_bytes(dtype, B: int, M: int, q_heads: int, cache, width: int) -> int:
+    """Bytes of workspace attend_trees needs for trees of M candidates and a table of `width` pages (0: none)."""
+    code = {torch.float32: F32, torch.bfloat16: BF16}[dtype]
+    return int(load().lantern_attend_trees_workspace_bytes(code, int(B), int(M), int(q_heads), ctypes.byref(_cache_args(cache)[0]), int(width)))
+
+
+def attend_trees(q, k, v, parent, cache, table, lengths, scale=None, workspace=None, stream=None):
+    """lantern_attend_trees: q [B, 1 + M, heads, D] and the rows' own k, v [B, 1 + M, key heads, D] over the cache and the
+    tree of parent int32[B*M] (None: every row follows the one before it).  scale: D ** -0.5 unless given.  workspace: a
+    uint8 tensor of at least attend_trees_workspace_bytes, or None to allocate one.  Returns out [B, 1 + M, heads, D]."""
+    lib = load()
+    c, parts = _cache_args(cache)
+    _rows_of_cache(c, k, v)
+    B, T = k.shape[:2]
+    if q.dim() != 4 or q.shape[:2] != k.shape[:2] or q.shape[3] != c.D or q.dtype != k.dtype or q.stride(3) != 1:
+        raise ValueError("q must be [B, rows, heads, D] like k and v, with dense heads")
+    _table_args(table, lengths, B)
+    if parent is not None and (parent.dtype != torch.int32 or parent.numel() != B * (T - 1) or not parent.is_contiguous()):
+        raise ValueError("parent must be a contiguous int32 tensor of B*M entries")
+    _need_here(stream, *parts, table, lengths, q, k, v, parent, workspace)
+    code, Hq, width = _dtype_code(q), q.shape[2], table.shape[1]
+    need = int(lib.lantern_attend_trees_workspace_bytes(code, B, T - 1, Hq, ctypes.byref(c), width))
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        _made_for(stream, workspace)
+    out = torch.empty((B, T, Hq, c.D), dtype=q.dtype, device=q.device)
+    _made_for(stream, out)
+    rc = lib.lantern_attend_trees(q.data_ptr(), _strides(*q.stride()[:3]), k.data_ptr(), _strides(*k.stride()[:3]), v.data_ptr(),
+                                  _strides(*v.stride()[:3]), code, B, T - 1, Hq, None if parent is None else parent.data_ptr(),
+                                  ctypes.byref(c), table.data_ptr(), width, lengths.data_ptr(),
+                                  c.D ** -0.5 if scale is None else float(scale), out.data_ptr(),
+                                  None if workspace is None else workspace.data_ptr(),
+                                  0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+    if rc != OK:
+        raise LanternError(rc, "lantern_attend_trees")
+    return out
+
+
+def prepare_cache(dtype, cache) -> None:
+    """lantern_prepare_cache: kernels and LDS limits of the three calls above for this dtype and cache, before a capture."""
+    rc = load().lantern_prepare_cache({torch.float32: F32, torch.bfloat16: BF16}[dtype], ctypes.byref(_cache_args(cache)[0]))
+    if rc != OK:
+        raise LanternError(rc, "lantern_prepare_cache")

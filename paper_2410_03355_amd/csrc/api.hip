@@ -1,9 +1,13 @@
 // C ABI of the library: argument validation on the host, then kernel launches.
 #include <hip/hip_runtime.h>
+#include <float.h>
 #include <limits.h>
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
+
+#include "cache_args.h"
 #include "knn_args.h"
 #include "lantern.h"
 #include "sequential_args.h"
@@ -392,6 +396,194 @@ int lantern_prepare(lantern_dtype logits_dtype, int V, int k) {
     if (e == hipSuccess) e = lantern::prepare_greedy((int)logits_dtype, V, k);
     if (e == hipSuccess) e = lantern::prepare_walks();
     if (e == hipSuccess) e = lantern::prepare_sequential((int)logits_dtype, V);
+    return e == hipSuccess ? LANTERN_OK : LANTERN_E_DEVICE;
+}
+
+namespace {
+
+bool aligned(const void* p, const lantern::Strided& s, int size) {   // every head's first element at a multiple of 16 bytes
+    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && s.seq * size % 16 == 0 && s.row * size % 16 == 0 && s.head * size % 16 == 0;
+}
+lantern::Strided strided(const int64_t* s) { return {s[0], s[1], s[2]}; }
+
+int cache_shape(const lantern_cache* c) {
+    if (!c) return LANTERN_E_NULL;
+    if (c->dtype != LANTERN_BF16 && c->dtype != LANTERN_E4M3) return LANTERN_E_DTYPE;
+    const int p = c->page_tokens, D = c->D;
+    if (c->pages < 1 || c->heads < 1 || c->heads > 65535 || (p != 16 && p != 32 && p != 64 && p != 128) ||
+        (D != 32 && D != 64 && D != 96 && D != 128))
+        return LANTERN_E_SHAPE;
+    return LANTERN_OK;
+}
+int cache_memory(const lantern_cache& c) {
+    if (!c.k || !c.v || (c.dtype == LANTERN_E4M3 && (!c.k_scale || !c.v_scale))) return LANTERN_E_NULL;
+    return ((reinterpret_cast<uintptr_t>(c.k) | reinterpret_cast<uintptr_t>(c.v)) & 15) == 0 ? LANTERN_OK : LANTERN_E_SHAPE;
+}
+int shift_of(int page_tokens) { return page_tokens == 16 ? 4 : page_tokens == 32 ? 5 : page_tokens == 64 ? 6 : 7; }
+
+// The rotation with nothing behind its last axis, and its number of pairs.
+int rotation_of(const lantern_rotation& r, int D, lantern_rotation* out, int* pairs) {
+    if (r.axes < 1 || r.axes > LANTERN_MAX_AXES) return LANTERN_E_SHAPE;
+    *out = r;
+    int64_t sum = 0;
+    for (int a = 0; a < LANTERN_MAX_AXES; ++a) {
+        if (a >= r.axes) out->pairs[a] = 0;
+        if (out->pairs[a] < 0) return LANTERN_E_SHAPE;
+        sum += out->pairs[a];
+    }
+    if (sum < 1 || 2 * sum > D) return LANTERN_E_SHAPE;
+    *pairs = (int)sum;
+    return r.positions && r.freqs ? LANTERN_OK : LANTERN_E_NULL;
+}
+
+int table_shape(const lantern_cache& c, int width) {
+    return width >= 1 && (int64_t)width * c.page_tokens <= INT_MAX ? LANTERN_OK : LANTERN_E_SHAPE;
+}
+
+int attend_plan(lantern_dtype dtype, int B, int M, int q_heads, const lantern_cache* cache, int width, lantern::AttendPlan* plan) {
+    if (!dtype_ok(dtype)) return LANTERN_E_DTYPE;
+    const int rc = cache_shape(cache);
+    if (rc != LANTERN_OK) return rc;
+    if (B < 0 || M < 0 || M > LANTERN_MAX_TREE || q_heads < 1 || q_heads % cache->heads || table_shape(*cache, width) != LANTERN_OK)
+        return LANTERN_E_SHAPE;
+    const int64_t group = q_heads / cache->heads;
+    if (group * (M + 1) > INT_MAX / 2 || (int64_t)B * q_heads > INT_MAX / (M + 1)) return LANTERN_E_SHAPE;
+    *plan = lantern::plan_attend(dtype, B, M, q_heads, *cache, width);
+    return ((int64_t)B * cache->heads * plan->splits + 8) * plan->row_tiles > INT_MAX ? LANTERN_E_SHAPE : LANTERN_OK;
+}
+
+}  // namespace
+
+int lantern_rotate_axes(const void* q, const int64_t* q_strides, int q_heads, const void* k, const int64_t* k_strides,
+                        int k_heads, lantern_dtype dtype, int N, int D, const lantern_rotation* rotation, int inverse,
+                        void* out_q, const int64_t* out_q_strides, void* out_k, const int64_t* out_k_strides,
+                        void* hip_stream) {
+    if (!dtype_ok(dtype)) return LANTERN_E_DTYPE;
+    if (N < 0 || q_heads < 1 || k_heads < 0 || D < 2 || D > LANTERN_MAX_HEAD || q_heads > INT_MAX - k_heads) return LANTERN_E_SHAPE;
+    if (N == 0) return LANTERN_OK;
+    if (!rotation) return LANTERN_E_NULL;
+    lantern::RotateArgs a;
+    const int rc = rotation_of(*rotation, D, &a.rot, &a.pairs);
+    if (rc != LANTERN_OK) return rc;
+    if (!q || !out_q || !q_strides || !out_q_strides) return LANTERN_E_NULL;
+    if (k_heads > 0 && (!k || !out_k || !k_strides || !out_k_strides)) return LANTERN_E_NULL;
+    a.N = N;
+    a.D = D;
+    a.q_heads = q_heads;
+    a.k_heads = k_heads;
+    a.inverse = inverse;
+    a.heads_per_block = 0;
+    a.q = q;
+    a.k = k;
+    a.out_q = out_q;
+    a.out_k = out_k;
+    a.sq = {0, q_strides[0], q_strides[1]};
+    a.soq = {0, out_q_strides[0], out_q_strides[1]};
+    a.sk = k_heads > 0 ? lantern::Strided{0, k_strides[0], k_strides[1]} : a.sq;
+    a.sok = k_heads > 0 ? lantern::Strided{0, out_k_strides[0], out_k_strides[1]} : a.soq;
+    const int size = dtype == LANTERN_F32 ? 4 : 2;
+    a.wide = a.pairs % 4 == 0 && D % 8 == 0 && aligned(q, a.sq, size) && aligned(out_q, a.soq, size) &&
+             (k_heads == 0 || (aligned(k, a.sk, size) && aligned(out_k, a.sok, size)));
+    const hipError_t e = lantern::launch_rotate_axes(a, dtype, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? LANTERN_OK : LANTERN_E_DEVICE;
+}
+
+int lantern_append_cache(const lantern_cache* cache, const int32_t* table, int table_width, const int32_t* lengths, int B,
+                         int T, const void* k, const int64_t* k_strides, const void* v, const int64_t* v_strides,
+                         lantern_dtype dtype, const lantern_rotation* rotation, const int32_t* path, const int32_t* count,
+                         int32_t* out_lengths, void* hip_stream) {
+    if (!dtype_ok(dtype)) return LANTERN_E_DTYPE;
+    int rc = cache_shape(cache);
+    if (rc != LANTERN_OK) return rc;
+    if (B < 0 || T < 1 || table_shape(*cache, table_width) != LANTERN_OK || (path && T < 2)) return LANTERN_E_SHAPE;
+    lantern::AppendArgs a;
+    a.touched = (int)std::min<int64_t>(table_width, ((int64_t)T + cache->page_tokens - 2) / cache->page_tokens + 1);
+    if ((int64_t)B * a.touched > INT_MAX || (int64_t)B * T > INT_MAX) return LANTERN_E_SHAPE;
+    if (B == 0) return LANTERN_OK;
+    a.pairs = 0;
+    a.rot = lantern_rotation{};
+    if (rotation) rc = rotation_of(*rotation, cache->D, &a.rot, &a.pairs);
+    if (rc != LANTERN_OK) return rc;
+    rc = cache_memory(*cache);
+    if (rc != LANTERN_OK) return rc;
+    if (!table || !lengths || !k || !v || !k_strides || !v_strides || !out_lengths || (path && !count)) return LANTERN_E_NULL;
+    if (out_lengths == lengths) return LANTERN_E_SHAPE;
+    a.cache = *cache;
+    a.page_shift = shift_of(cache->page_tokens);
+    a.table = table;
+    a.lengths = lengths;
+    a.width = table_width;
+    a.B = B;
+    a.T = T;
+    a.k = k;
+    a.v = v;
+    a.sk = strided(k_strides);
+    a.sv = strided(v_strides);
+    const int size = dtype == LANTERN_F32 ? 4 : 2;
+    a.wide_k = a.pairs % 4 == 0 && aligned(k, a.sk, size);
+    a.wide_v = aligned(v, a.sv, size);
+    a.path = path;
+    a.count = count;
+    a.out_lengths = out_lengths;
+    const hipError_t e = lantern::launch_append_cache(a, dtype, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? LANTERN_OK : LANTERN_E_DEVICE;
+}
+
+size_t lantern_attend_trees_workspace_bytes(lantern_dtype dtype, int B, int M, int q_heads, const lantern_cache* cache,
+                                            int table_width) {
+    lantern::AttendPlan plan;
+    return attend_plan(dtype, B, M, q_heads, cache, table_width, &plan) == LANTERN_OK && B > 0 ? plan.workspace : 0;
+}
+
+int lantern_attend_trees(const void* q, const int64_t* q_strides, const void* k, const int64_t* k_strides, const void* v,
+                         const int64_t* v_strides, lantern_dtype dtype, int B, int M, int q_heads, const int32_t* parent,
+                         const lantern_cache* cache, const int32_t* table, int table_width, const int32_t* lengths,
+                         float scale, void* out, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    lantern::AttendPlan plan;
+    int rc = attend_plan(dtype, B, M, q_heads, cache, table_width, &plan);
+    if (rc != LANTERN_OK) return rc;
+    if (!(scale >= 0.f) || scale > FLT_MAX) return LANTERN_E_SHAPE;
+    if (B == 0) return LANTERN_OK;
+    rc = cache_memory(*cache);
+    if (rc != LANTERN_OK) return rc;
+    if (!q || !k || !v || !q_strides || !k_strides || !v_strides || !table || !lengths || !out) return LANTERN_E_NULL;
+    if (plan.workspace && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < plan.workspace))
+        return LANTERN_E_WORKSPACE;
+    lantern::AttendArgs a;
+    a.cache = *cache;
+    a.page_shift = shift_of(cache->page_tokens);
+    a.table = table;
+    a.lengths = lengths;
+    a.parent = parent;
+    a.width = table_width;
+    a.B = B;
+    a.M = M;
+    a.q_heads = q_heads;
+    a.group = q_heads / cache->heads;
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.sq = strided(q_strides);
+    a.sk = strided(k_strides);
+    a.sv = strided(v_strides);
+    const int size = dtype == LANTERN_F32 ? 4 : 2;
+    a.wide = aligned(q, a.sq, size) && aligned(k, a.sk, size);
+    a.scale = (float)((double)scale * 1.4426950408889634074);
+    a.out = out;
+    a.part = static_cast<float*>(workspace);
+    a.splits = plan.splits;
+    a.row_tiles = plan.row_tiles;
+    const hipError_t e = lantern::launch_attend_trees(a, dtype, plan.query_tiles, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? LANTERN_OK : LANTERN_E_DEVICE;
+}
+
+int lantern_prepare_cache(lantern_dtype dtype, const lantern_cache* cache) {
+    if (!dtype_ok(dtype)) return LANTERN_E_DTYPE;
+    const int rc = cache_shape(cache);
+    if (rc != LANTERN_OK) return rc;
+    hipError_t e = lantern::prepare_rotate(dtype);
+    if (e == hipSuccess) e = lantern::prepare_append(dtype, *cache);
+    if (e == hipSuccess) e = lantern::prepare_attend(dtype, *cache);
     return e == hipSuccess ? LANTERN_OK : LANTERN_E_DEVICE;
 }
 

@@ -1,0 +1,67 @@
+// Arguments of the kernels around a tree step (rotate.hip, append.hip, attend.hip), as api.hip hands them over after its checks.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "lantern.h"
+
+namespace lantern {
+
+struct Strided {            // elements from one sequence, row and head to the next; a head's elements are dense
+    int64_t seq, row, head;
+};
+
+struct RotateArgs {
+    lantern_rotation rot;
+    int pairs;              // of all axes
+    int N, D, q_heads, k_heads, inverse;
+    int heads_per_block;
+    bool wide;              // vector loads and stores
+    const void *q, *k;
+    void *out_q, *out_k;
+    Strided sq, sk, soq, sok;
+};
+
+struct AppendArgs {
+    lantern_cache cache;
+    lantern_rotation rot;
+    int pairs;              // 0: keys are stored as they are
+    int page_shift;
+    const int32_t *table, *lengths;
+    int width, B, T, touched;   // touched: most pages that one sequence's rows reach
+    bool wide_k, wide_v;
+    const void *k, *v;
+    Strided sk, sv;
+    const int32_t *path, *count;
+    int32_t* out_lengths;
+};
+
+struct AttendArgs {
+    lantern_cache cache;
+    int page_shift;
+    const int32_t *table, *lengths, *parent;
+    int width, B, M, q_heads, group;   // group: query heads to a key head
+    bool wide;
+    const void *q, *k, *v;
+    Strided sq, sk, sv;
+    float scale;            // of the scores, times log2(e)
+    void* out;              // [B, M + 1, q_heads, D]
+    float* part;            // of `splits` parts: their outputs [splits, rows, D], maxima and sums [splits, rows]
+    int splits, row_tiles;
+};
+
+struct AttendPlan {
+    int splits, row_tiles, query_tiles;
+    size_t workspace;
+};
+AttendPlan plan_attend(int dtype, int B, int M, int q_heads, const lantern_cache& c, int width);
+
+hipError_t launch_rotate_axes(const RotateArgs& a, int dtype, hipStream_t stream);
+hipError_t launch_append_cache(const AppendArgs& a, int dtype, hipStream_t stream);
+hipError_t launch_attend_trees(const AttendArgs& a, int dtype, int query_tiles, hipStream_t stream);
+hipError_t prepare_rotate(int dtype);
+hipError_t prepare_append(int dtype, const lantern_cache& c);
+hipError_t prepare_attend(int dtype, const lantern_cache& c);
+
+}  // namespace lantern
