@@ -541,9 +541,11 @@ typedef struct {
  *      value is its code times the scale of its page and head (else not read)
  *   dtype        LANTERN_BF16 or LANTERN_E4M3
  *   page_tokens  16, 32, 64 or 128;  D  32, 64, 96 or 128;  heads <= 65535
- * k and v are 16-byte aligned.  The struct itself lies in host memory and is
+ * k and v are 16-byte aligned; a page table has room for LANTERN_MAX_TOKENS tokens
+ * of a sequence at most.  The struct itself lies in host memory and is
  * read during the call.
  */
+#define LANTERN_MAX_TOKENS (1 << 30)
 typedef struct {
     void* k;
     void* v;
@@ -601,8 +603,8 @@ int lantern_rotate_axes(const void* q, const int64_t* q_strides, int q_heads, co
  * pages keep infinities).  Slots behind the new length keep what they hold.
  * Pages written here must belong to one sequence of the call alone, and the
  * rows must not overlap the cache.
- * Errors: E_DTYPE, E_SHAPE (limits above; B < 0, T < 1, table_width < 1 or more
- * tokens than INT_MAX, path without T > 1, B * touched pages beyond INT_MAX,
+ * Errors: E_DTYPE, E_SHAPE (limits above; B < 0, T < 1, table_width < 1 or too
+ * many tokens, path without T > 1, B * touched pages beyond INT_MAX,
  * out_lengths == lengths), E_NULL (also path without count), E_DEVICE.  B = 0 does nothing.
  */
 int lantern_append_cache(const lantern_cache* cache, const int32_t* table, int table_width, const int32_t* lengths, int B,
@@ -644,7 +646,7 @@ int lantern_append_cache(const lantern_cache* cache, const int32_t* table, int t
  * formed in binary32 throughout; with BF16 the weights (times the values' scale)
  * are rounded to bfloat16 for the second product, half a step of 2^-8 each.
  * Errors: E_DTYPE, E_SHAPE (B < 0, M < 0, M > LANTERN_MAX_TREE, q_heads not a
- * positive multiple of the cache's heads, table_width < 1 or more tokens than INT_MAX, the
+ * positive multiple of the cache's heads, table_width < 1 or too many tokens, the
  * cache's limits, scale not finite or negative, more workgroups or rows than INT_MAX),
  * E_NULL, E_WORKSPACE, E_DEVICE.  B = 0 does nothing.
  */

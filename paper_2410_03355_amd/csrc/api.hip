@@ -437,7 +437,7 @@ int rotation_of(const lantern_rotation& r, int D, lantern_rotation* out, int* pa
 }
 
 int table_shape(const lantern_cache& c, int width) {
-    return width >= 1 && (int64_t)width * c.page_tokens <= INT_MAX ? LANTERN_OK : LANTERN_E_SHAPE;
+    return width >= 1 && (int64_t)width * c.page_tokens <= LANTERN_MAX_TOKENS ? LANTERN_OK : LANTERN_E_SHAPE;
 }
 
 int attend_plan(lantern_dtype dtype, int B, int M, int q_heads, const lantern_cache* cache, int width, lantern::AttendPlan* plan) {
@@ -567,13 +567,17 @@ int lantern_attend_trees(const void* q, const int64_t* q_strides, const void* k,
     a.sk = strided(k_strides);
     a.sv = strided(v_strides);
     const int size = dtype == LANTERN_F32 ? 4 : 2;
-    a.wide = aligned(q, a.sq, size) && aligned(k, a.sk, size);
+    a.wide = aligned(q, a.sq, size) && aligned(k, a.sk, size) && aligned(v, a.sv, size);
     a.scale = (float)((double)scale * 1.4426950408889634074);
     a.out = out;
     a.part = static_cast<float*>(workspace);
     a.splits = plan.splits;
     a.row_tiles = plan.row_tiles;
-    const hipError_t e = lantern::launch_attend_trees(a, dtype, plan.query_tiles, static_cast<hipStream_t>(hip_stream));
+    a.by_tiles = lantern::Divisor(plan.row_tiles);
+    a.by_splits = lantern::Divisor(plan.splits);
+    a.by_heads = lantern::Divisor(cache->heads);
+    a.by_group = lantern::Divisor(a.group);
+    const hipError_t e = lantern::launch_attend_trees(a, dtype, plan.row_group, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? LANTERN_OK : LANTERN_E_DEVICE;
 }
 

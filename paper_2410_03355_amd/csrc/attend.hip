@@ -3,8 +3,8 @@
 // Row i of a sequence (0: the token before the candidates, 1 + j: candidate j) sees the cached tokens and, of the sequence's
 // own rows, itself and its ancestors:  o = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale * q . k_j - m).
 //
-// One wavefront takes up to 64 rows (QT tiles of 16; the query heads of a key head are rows of one matrix) through a run of
-// cached tokens, one pass, with the running maximum and sum of the softmax.  Both products keep to registers:
+// One wavefront takes 16 or 32 rows (QT tiles of 16; the query heads of a key head are rows of one matrix) through a run of
+// cached tokens, one pass, with the running maximum and sum of the softmax.  Scores and weights keep to registers:
 //   S^T = K Q^T    A: 16 tokens by 32 of the head's elements, B: the same elements of 16 rows
 //   O^T = V^T P^T  A: 16 elements by 32 tokens, B: the same tokens of 16 rows
 // The result of an instruction has a row's scores of four tokens in each lane, and the second product wants a row's weights of
@@ -15,6 +15,7 @@
 // The four wavefronts of a workgroup take every fourth tile of tokens each and join through LDS; where sequences, heads and
 // row tiles are too few to fill the device a sequence is split over workgroups as well, whose parts a second kernel joins.
 #include <hip/hip_runtime.h>
+#include <float.h>
 #include <limits.h>
 #include <stdint.h>
 
@@ -22,12 +23,14 @@
 
 #include "cache_args.h"
 #include "device_utils.h"
+#include "lds_limit.h"
 #include "rotation.h"
 
 namespace lantern {
 
 constexpr int MOST_ROWS = LANTERN_MAX_TREE + 1;   // of a sequence
-constexpr int WORDS = MOST_ROWS / 32;
+// Of the lambdas: into their one caller before anything else is done with them, so that what they are handed stays in registers.
+#define INLINE __attribute__((always_inline))
 constexpr float LAZY = 8.f;      // a row's maximum moves up only when a score passes it by 2^8: weights stay under 2^8
 
 struct F32x8 {
@@ -48,16 +51,17 @@ __device__ __forceinline__ f32x4 mma(const F32x8& a, const F32x8& b, f32x4 c) {
 }
 
 // Eight cached values as an operand; both types of a cache are exact in both types of an operand.
+// (bf16: times a power of two, for nothing).
 template <typename T>
-__device__ __forceinline__ typename Frag<T>::type from_e4m3(unsigned lo, unsigned hi);
+__device__ __forceinline__ typename Frag<T>::type from_e4m3(unsigned lo, unsigned hi, float by = 1.f);
 template <>
-__device__ __forceinline__ bf16x8 from_e4m3<bf16>(unsigned lo, unsigned hi) {
-    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
-    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
+__device__ __forceinline__ bf16x8 from_e4m3<bf16>(unsigned lo, unsigned hi, float by) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, by, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, by, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, by, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, by, true);
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 template <>
-__device__ __forceinline__ F32x8 from_e4m3<float>(unsigned lo, unsigned hi) {
+__device__ __forceinline__ F32x8 from_e4m3<float>(unsigned lo, unsigned hi, float) {
     const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)lo, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)lo, true);
     const f32x2 c = __builtin_amdgcn_cvt_pk_f32_fp8((int)hi, false), d = __builtin_amdgcn_cvt_pk_f32_fp8((int)hi, true);
     return F32x8{{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]}};
@@ -79,6 +83,9 @@ __device__ __forceinline__ F32x8 from_bf16<float>(u32x4 w) {
 __device__ __forceinline__ void set(bf16x8& f, int i, float x) { f[i] = (bf16)x; }
 __device__ __forceinline__ void set(F32x8& f, int i, float x) { f.x[i] = x; }
 
+__device__ __forceinline__ float get(const bf16x8& f, int i) { return (float)f[i]; }
+__device__ __forceinline__ float get(const F32x8& f, int i) { return f.x[i]; }
+
 // Eight elements in a row of a dense tensor.
 __device__ __forceinline__ bf16x8 load8(const bf16* x, bool wide) {
     if (wide) return *reinterpret_cast<const bf16x8*>(x);
@@ -92,154 +99,84 @@ __device__ __forceinline__ F32x8 load8(const float* x, bool wide) {
     return F32x8{{x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]}};
 }
 
+// Over the four lane groups: the swaps leave a value's partner of 16, then of 32 lanes on in the other register.
 __device__ __forceinline__ float over_groups_max(float x) {
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 __device__ __forceinline__ float over_groups_sum(float x) {
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// A tile of cached tokens on its way: keys as the first product's A, values as the second's.
+// A tile of cached tokens: 4 * CH of them, of which lane group g holds the values of CH.
+//
+// Neighbouring lanes of a product want neighbouring tokens of the keys and neighbouring elements of the values, and those lie
+// 32 .. 256 bytes apart in a page: a load in that order costs the address unit one access per lane (48 to 51 per instruction were counted,
+// and the unit was busy all the time).  So a team of wavefronts brings a tile to LDS in the order of memory, 16 bytes to a lane, and
+// the products read it from there; with four wavefronts to a team that is also one load for all of them.  Rows of LDS end with
+// 16 bytes more, and keys stand in the order of the product's rows, so that 16 lanes meet 16 different groups of banks.
 template <bool EIGHT, int D>
 struct Tile {
-    static constexpr int CH = EIGHT ? 16 : 8;          // tokens to a lane group
+    static constexpr int CH = EIGHT ? 16 : 8;          // 16 bytes of an element's values
     static constexpr int TOKENS = 4 * CH;
-    static constexpr int SUB = CH / 4;                 // tiles of 16 tokens
-    static constexpr int KW = EIGHT ? D / 16 : D / 8;  // words of a token's key in a lane
-    unsigned k[SUB][KW];
-    u32x4 v[D / 16];
-    float f, vs;                                       // scale of this lane's scores, and of its values
+    static constexpr int SIZE = EIGHT ? 1 : 2;
+    static constexpr int CHUNKS = 4 * D;               // of 16 bytes, of its keys as of its values
+    static constexpr int PER_TOKEN = D * SIZE / 16;    // of them a token's key
+    static constexpr int PARTS = TOKENS / 16;          // most pages that it lies on
+    static constexpr int KROW = D * SIZE + 16, VROW = 64 + 16;
+    static constexpr int KBYTES = TOKENS * KROW, VBYTES = D * VROW;
+    // Whether 64 chunks in a row lie on one page, however small
+    static constexpr bool WHOLE = 16 * D * SIZE % 1024 == 0;
 
     // Where the eight elements of step s (of 32) begin in a lane group: a load of 16 bytes brings two steps of 8-bit keys.
     __device__ static __forceinline__ int element(int s, int g) {
         if (EIGHT && s < D / 64 * 2) return s / 2 * 64 + g * 16 + s % 2 * 8;
         return s * 32 + g * 8;
     }
-
-    template <typename T>
-    __device__ __forceinline__ typename Frag<T>::type key(int t, int s) const {
-        if constexpr (EIGHT) return from_e4m3<T>(k[t][2 * s], k[t][2 * s + 1]);
-        else return from_bf16<T>(u32x4{k[t][4 * s], k[t][4 * s + 1], k[t][4 * s + 2], k[t][4 * s + 3]});
-    }
-    template <typename T>
-    __device__ __forceinline__ typename Frag<T>::type value(int dt, int p) const {
-        if constexpr (EIGHT) return from_e4m3<T>(v[dt][2 * p], v[dt][2 * p + 1]);
-        else return from_bf16<T>(v[dt]);
-    }
-    // Nothing of the values from the lane's `keep`-th on: the slots behind a sequence's end hold anything, NaN too.
-    __device__ __forceinline__ void cut_values(int keep) {
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const int in = min(4, max(0, (keep * (EIGHT ? 1 : 2)) - 4 * w));     // bytes of this word
-            const unsigned mask = in == 4 ? 0xFFFFFFFFu : (1u << 8 * in) - 1u;
-#pragma unroll
-            for (int dt = 0; dt < D / 16; ++dt) v[dt][w] &= mask;
-        }
-    }
+    // Row of a token's key in LDS: tile t of 16, row i of that, for token CH * (i / 4) + 4 t + i % 4.
+    __device__ static __forceinline__ int row_of(int token) { return token % CH / 4 * 16 + token / CH * 4 + token % 4; }
 };
 
-// Pages of a tile, asked for one tile ahead of its tokens.
-struct PageIds {
-    int k, v;
-};
-
-template <typename T, bool EIGHT, int D, int QT>
-__global__ __launch_bounds__(NT, 1) void attend_trees_kernel(AttendArgs a) {
-    typedef Tile<EIGHT, D> Tokens;
+// What one wavefront keeps of its QT * 16 rows: lane col of every group holds row col of a tile.
+template <typename T, int D, int QT>
+struct Rows {
     typedef typename Frag<T>::type Operand;
-    constexpr int CH = Tokens::CH, TOKENS = Tokens::TOKENS, SUB = Tokens::SUB, STEPS = D / 32, DT = D / 16;
-    constexpr int RED = 16 * (D + 4);                      // floats of one wavefront's part of 16 rows
-    constexpr int SHARED = NW * RED > MOST_ROWS * WORDS ? NW * RED : MOST_ROWS * WORDS;
-    __shared__ __attribute__((aligned(16))) float shared[SHARED];   // first the rows' ancestors, then the wavefronts' parts
-    __shared__ int jump[MOST_ROWS], lost[MOST_ROWS];
-    __shared__ float wave_m[NW][16 * QT], wave_l[NW][16 * QT];
-
-    const int lane = threadIdx.x & (WAVE - 1), wave = threadIdx.x / WAVE, col = lane & 15, g = lane >> 4;
-    const int rows_of = a.M + 1, R = rows_of * a.group, heads = a.cache.heads;
-    // The row tiles of one part of a sequence and head read the same tokens: they get numbers 8 apart, which one XCD serves.
-    const int parts = a.B * heads * a.splits, per = 8 * a.row_tiles;
-    const int part = (int)blockIdx.x / per * 8 + (int)blockIdx.x % 8, row_tile = (int)blockIdx.x % per / 8;
-    if (part >= parts) return;
-    const int split = part % a.splits, bh = part / a.splits, b = bh / heads, h = bh % heads;
-    const int first_row = row_tile * 16 * QT;
-    const int told = a.lengths[b], page = 1 << a.page_shift;
-    const bool absent = told < 0, too_long = (int64_t)told > (int64_t)a.width << a.page_shift;
-    const int length = absent || too_long ? 0 : told;
-    const bool has_tree = split == a.splits - 1;
-
-    // ---- ancestors of every row, itself included, as bits: doubling along the parents
-    unsigned* seen = reinterpret_cast<unsigned*>(shared);
-    if (has_tree) {
-        const int i = threadIdx.x;
-        if (i < rows_of) {
-            int up = 0, bad = absent;
-            if (i > 0) {
-                const int p = a.parent ? a.parent[(int64_t)b * a.M + i - 1] : i - 2;
-                if (p < -1 || p >= i - 1) bad = 1;
-                else up = p + 1;
-            }
-            for (int w = 0; w < WORDS; ++w) seen[i * WORDS + w] = w == i / 32 ? 1u << i % 32 : 0u;
-            jump[i] = up;
-            lost[i] = bad;
-        }
-        __syncthreads();
-        for (;;) {
-            unsigned got[WORDS];
-            int to = 0, bad = 0;
-            if (i < rows_of) {
-                const int j = jump[i];
-                for (int w = 0; w < WORDS; ++w) got[w] = seen[j * WORDS + w];
-                bad = lost[j];
-                to = jump[j];
-            }
-            const int more = __syncthreads_or(i < rows_of && jump[i] != 0);
-            if (i < rows_of) {
-                for (int w = 0; w < WORDS; ++w) seen[i * WORDS + w] |= got[w];
-                lost[i] |= bad;
-                jump[i] = to;
-            }
-            __syncthreads();
-            if (!more) break;
-        }
-    }
-
-    // ---- the rows: B of the first product
+    static constexpr int DT = D / 16, STEPS = D / 32;
+    // bf16 weights are summed as they are rounded, by the same instructions: a row of ones above the values.  fp32: in the lanes.
+    static constexpr bool ONES = sizeof(T) == 2;
     Operand q[QT][STEPS];
+    f32x4 o[QT][DT], sums[QT];
+    float m[QT];                   // running maximum, the same in all groups
+
+    __device__ __forceinline__ void begin() {
 #pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-        const int r = min(first_row + qt * 16 + col, R - 1), node = r / a.group, head = h * a.group + r % a.group;
-        const T* x = static_cast<const T*>(a.q) + b * a.sq.seq + node * a.sq.row + head * a.sq.head;
+        for (int qt = 0; qt < QT; ++qt) {
+            m[qt] = neg_inf_f();
+            sums[qt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) q[qt][s] = load8(x + Tokens::element(s, g), a.wide);
+            for (int dt = 0; dt < DT; ++dt) o[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
     }
-    f32x4 o[QT][DT];
-    float m[QT], l[QT];
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-        m[qt] = neg_inf_f();
-        l[qt] = 0.f;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    __device__ __forceinline__ float sum(int qt) const {
+        return ONES ? sums[qt][0] : over_groups_sum((sums[qt][0] + sums[qt][1]) + (sums[qt][2] + sums[qt][3]));
     }
 
-    // Scores -> weights of one tile.  s: the scores, f: their scale (>= 0) in this lane, vs: the values'.  vis[qt]: bit c, whether
-    // the row sees token c of the lane's CH.
-    auto weigh = [&](f32x4 (&s)[QT][SUB], float f, float vs, const unsigned (&vis)[QT], bool masked, Operand (&p)[QT][CH / 8]) {
+    // Scores of 32 tokens -> weights.  f > 0: the scores' scale in this lane; vs: what the weights are multiplied by for the second product.
+    // Tokens that are not seen have a score of -inf.
+    __device__ __forceinline__ void weigh(const f32x4 (&s)[QT][2], float f, float vs, Operand (&p)[QT]) {
         float top[QT];
         bool up = false;
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) {
-            float x = neg_inf_f();
+            float x = s[qt][0][0];
 #pragma unroll
-            for (int t = 0; t < SUB; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    if (masked && !(vis[qt] >> (4 * t + r) & 1)) s[qt][t][r] = neg_inf_f();
-                    x = fmaxf(x, s[qt][t][r]);
-                }
-            top[qt] = x == neg_inf_f() ? x : x * f;
+            for (int j = 1; j < 8; ++j) x = fmaxf(x, s[qt][j / 4][j % 4]);
+            top[qt] = x * f;
             up |= top[qt] > m[qt] + LAZY;
         }
         if (__any(up)) {
@@ -248,255 +185,562 @@ __global__ __launch_bounds__(NT, 1) void attend_trees_kernel(AttendArgs a) {
                 const float to = fmaxf(m[qt], over_groups_max(top[qt]));
                 const float by = to == m[qt] ? 1.f : __builtin_amdgcn_exp2f(m[qt] - to);
                 m[qt] = to;
-                l[qt] *= by;
+                sums[qt] *= by;
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) o[qt][dt] *= by;
             }
         }
+        const bool scaled = __any(vs != 1.f);
+        Operand one;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) set(one, i, 1.f);
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) {
             const float less = m[qt] == neg_inf_f() ? 0.f : -m[qt];
+            float w[8];
 #pragma unroll
-            for (int t = 0; t < SUB; ++t)
+            for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][j / 4][j % 4], f, less));
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qt][t][r], f, less));
-                    if (masked && !(vis[qt] >> (4 * t + r) & 1)) w = 0.f;
-                    l[qt] += w;
-                    // bf16: a weight times its value's scale is rounded once, by 2^-9 of it at most, as an output is
-                    set(p[qt][t / 2], t % 2 * 4 + r, EIGHT ? w * vs : w);
-                }
+            for (int j = 0; j < 8; ++j) set(p[qt], j, w[j]);
+            if constexpr (ONES) {
+                sums[qt] = mma(one, p[qt], sums[qt]);
+            } else {
+                sums[qt][0] += w[0] + w[1];
+                sums[qt][1] += w[2] + w[3];
+                sums[qt][2] += w[4] + w[5];
+                sums[qt][3] += w[6] + w[7];
+            }
+            if (scaled) {      // bf16: rounded once all the same, from fp32
+#pragma unroll
+                for (int j = 0; j < 8; ++j) set(p[qt], j, w[j] * vs);
+            }
+        }
+    }
+};
+
+// What other lanes of the wavefront have written to LDS is there.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// LDS of a workgroup: a place for each wavefront's tile, which keys and then values go through; own rows, as many as a tile has tokens:
+// their keys like a tile's, their values turned over; what the rows see.  In the end the wavefronts' parts.
+template <typename T, bool EIGHT, int D, int QT>
+struct Shared {
+    typedef Tile<EIGHT, D> Tokens;
+    static constexpr int TILE = Tokens::KBYTES > Tokens::VBYTES ? Tokens::KBYTES : Tokens::VBYTES;
+    static constexpr int OWN_KROW = D * (int)sizeof(T) + 16, OWN_VROW = Tokens::TOKENS + 16 / (int)sizeof(T);
+    static constexpr int OWN_K = Tokens::TOKENS * OWN_KROW, OWN_V = (int)sizeof(T) * D * OWN_VROW;
+    static constexpr int FIXED = NW * TILE + OWN_K + OWN_V;
+    static constexpr int PART = 16 * QT * (D + 4);                  // floats of a wavefront's part
+    static constexpr int JOIN = NW * PART * (int)sizeof(float);
+    __host__ __device__ static constexpr int bytes(int rows) {      // seen, present; jump, lost where rows are over 64
+        const int words = (rows + 31) / 32;
+        const int all = FIXED + (int)sizeof(int) * (rows * words + words + (rows > WAVE ? 2 * rows : 0));
+        return all > JOIN ? all : JOIN;
+    }
+};
+
+// Four wavefronts take the same QT * 16 rows, each through every fourth tile of a sequence's cached tokens.
+template <typename T, bool EIGHT, int D, int QT>
+__global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_trees_kernel(AttendArgs a) {
+    typedef Rows<T, D, QT> Mine;
+    typedef Tile<EIGHT, D> Tokens;
+    typedef Shared<T, EIGHT, D, QT> Lds;
+    typedef typename Frag<T>::type Operand;
+    constexpr int CH = Tokens::CH, TOKENS = Tokens::TOKENS, STEPS = D / 32, DT = D / 16, SIZE = Tokens::SIZE, HALVES = CH / 8;
+    constexpr int ROW = Lds::OWN_VROW, PARTS = Tokens::PARTS;
+    constexpr int PER = Tokens::CHUNKS / WAVE;      // chunks of a tile to a lane
+    extern __shared__ __attribute__((aligned(16))) char shared[];
+    __shared__ float wave_m[NW][16 * QT], wave_l[NW][16 * QT];
+
+    const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), col = lane & 15, g = lane >> 4;
+    const int rows_of = a.M + 1, words = (rows_of + 31) / 32, R = rows_of * a.group, heads = a.cache.heads;
+    char* const own_keys = shared + NW * Lds::TILE;
+    T* const staged = reinterpret_cast<T*>(own_keys + Lds::OWN_K);
+    unsigned* const seen = reinterpret_cast<unsigned*>(shared + Lds::FIXED);
+    unsigned* const present = seen + rows_of * words;
+    int *const jump = reinterpret_cast<int*>(present + words), *const lost = jump + rows_of;
+    // The row tiles of one part of a sequence and head read the same tokens: they get numbers 8 apart, which one XCD serves.
+    const int chunk = a.by_tiles.of(blockIdx.x >> 3);
+    const int part = chunk * 8 + (int)(blockIdx.x & 7), first_row = ((int)(blockIdx.x >> 3) - chunk * a.row_tiles) * 16 * QT;
+    if (part >= a.B * heads * a.splits) return;
+    const int bh = a.by_splits.of(part), split = part - bh * a.splits, b = a.by_heads.of(bh), h = bh - b * heads;
+    const int told = a.lengths[b], page = 1 << a.page_shift;
+    const bool absent = told < 0, too_long = (int64_t)told > (int64_t)a.width << a.page_shift;
+    const int length = absent || too_long ? 0 : told;
+    const bool has_tree = split == a.splits - 1;
+
+    // ---- the rows: B of the first product
+    Mine mine;
+    int node[QT];      // the sequence's row that a row of the matrix belongs to
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) node[qt] = a.by_group.of(min(first_row + qt * 16 + col, R - 1));
+    auto rows = [&](bool wide) INLINE {
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+            const int head = h * a.group + min(first_row + qt * 16 + col, R - 1) - node[qt] * a.group;
+            const T* x = static_cast<const T*>(a.q) + b * a.sq.seq + node[qt] * a.sq.row + head * a.sq.head;
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) mine.q[qt][s] = load8(x + Tokens::element(s, g), wide);
         }
     };
+    if (a.wide) rows(true);
+    else rows(false);
+    mine.begin();
 
-    // ---- cached tokens
+    // ---- where the cached tokens are
     const int tiles = (length + TOKENS - 1) / TOKENS;
-    const int begin = (int)((int64_t)tiles * split / a.splits) + wave, end = (int)((int64_t)tiles * (split + 1) / a.splits);
-    const int32_t* table = a.table + (int64_t)b * a.width;
-    const int last_page = (length - 1) >> a.page_shift;
-    const int64_t page_bytes = (int64_t)heads * page * D * (EIGHT ? 1 : 2);
-    const char* kbase = static_cast<const char*>(a.cache.k) + (int64_t)h * page * D * (EIGHT ? 1 : 2);
-    const char* vbase = static_cast<const char*>(a.cache.v) + (int64_t)h * page * D * (EIGHT ? 1 : 2);
-
-    auto pages_of = [&](int tile) {      // a group behind the end is given the last page, whose tokens are then not seen
-        const int kt = tile * TOKENS + col / 4 * CH, vt = tile * TOKENS + g * CH;
-        return PageIds{table[min(kt >> a.page_shift, last_page)], table[min(vt >> a.page_shift, last_page)]};
+    // tiles * splits stays under 2^31 (plan_attend); one part begins at 0 whatever the length
+    const int begin = a.splits == 1 ? wave : a.by_splits.of(tiles * split) + wave;
+    const int end = a.splits == 1 ? tiles : a.by_splits.of(tiles * (split + 1));
+    const int last = begin < end ? begin + (end - 1 - begin) / NW * NW : begin;      // this wavefront's last tile
+    const int32_t* const table = a.table + (int64_t)b * a.width;
+    const unsigned page_bytes = (unsigned)heads * page * D * SIZE;      // 65535 heads at most: under 2^31
+    const char* const kbase = static_cast<const char*>(a.cache.k) + (int64_t)h * page * D * SIZE;
+    const char* const vbase = static_cast<const char*>(a.cache.v) + (int64_t)h * page * D * SIZE;
+    // This lane's chunks of a tile: page of the tile's, place in it, place in LDS; each a lane's own part and, where a load's 64 chunks
+    // are whole tokens (elements) of one page, one that the wavefront shares.
+    constexpr bool LINEAR = Tokens::WHOLE && WAVE % Tokens::PER_TOKEN == 0;
+    const int row_chunks = page * SIZE >= 64 ? 2 : page * SIZE >= 32 ? 1 : 0;      // log2 of an element's chunks on one page
+    struct Chunk {
+        int part, from, to, token;
     };
-    auto bring = [&](int tile, PageIds id, Tokens& x) {
-        const bool good_k = id.k >= 0 && id.k < a.cache.pages, good_v = id.v >= 0 && id.v < a.cache.pages;
-        const int kpage = good_k ? id.k : 0, vpage = good_v ? id.v : 0;
-        const int kslot = ((tile * TOKENS + col / 4 * CH) & (page - 1)) + col % 4, vslot = (tile * TOKENS + g * CH) & (page - 1);
-        const char* kp = kbase + kpage * page_bytes + (int64_t)kslot * D * (EIGHT ? 1 : 2);
-        const char* vp = vbase + vpage * page_bytes + vslot * (EIGHT ? 1 : 2);
+    auto key_chunk = [&](int j) INLINE {
+        constexpr int AT_ONCE = WAVE / Tokens::PER_TOKEN;      // tokens to a load
+        if constexpr (LINEAR) {
+            const int first = j * AT_ONCE, mine = lane / Tokens::PER_TOKEN;
+            return Chunk{first >> a.page_shift, (first & (page - 1)) * (D * SIZE) + lane * 16,
+                         (Tokens::row_of(first + mine) * Tokens::KROW) + lane % Tokens::PER_TOKEN * 16, first};
+        } else {
+            const int c = lane + j * WAVE, token = c / Tokens::PER_TOKEN, ch = c % Tokens::PER_TOKEN;
+            return Chunk{token >> a.page_shift, (token & (page - 1)) * (D * SIZE) + ch * 16, Tokens::row_of(token) * Tokens::KROW + ch * 16, token};
+        }
+    };
+    auto value_chunk = [&](int j) INLINE {
+        if constexpr (LINEAR) {
+            const int first = j * (WAVE >> row_chunks), d = first % D, part = first / D;
+            const int mine = lane >> row_chunks, gi = lane & ((1 << row_chunks) - 1);
+            return Chunk{part, d * page * SIZE + (mine * page * SIZE + gi * 16),
+                         d * Tokens::VROW + (part << row_chunks) * 16 + (mine * Tokens::VROW + gi * 16), ((part << row_chunks) + gi) * CH};
+        } else {
+            const int x = (lane + j * WAVE) >> row_chunks, gi = lane & ((1 << row_chunks) - 1), part = x / D, d = x % D;
+            return Chunk{part, d * page * SIZE + gi * 16, d * Tokens::VROW + ((part << row_chunks) + gi) * 16, ((part << row_chunks) + gi) * CH};
+        }
+    };
+    // Pages of a tile, in the lanes of one load that is asked for a tile ahead and without waiting for the length.
+    auto ask_ids = [&](int tile) INLINE { return table[min((tile * TOKENS >> a.page_shift) + lane % PARTS, a.width - 1)]; };
+    auto good = [&](int id) INLINE { return (unsigned)id < (unsigned)a.cache.pages; };
+    // One of the up to four of a tile.  A page behind the end is not looked at (page 0 is read in its place, and its tokens are not
+    // seen); nor is one that is no page.
+    struct Pages {
+        uint64_t a, b, c, d;
+        __device__ __forceinline__ uint64_t operator[](int i) const {
+            const uint64_t p = a, q = b, r = c, s = d;      // values first: a choice of members is one of addresses, in scratch memory
+            const uint64_t low = i & 1 ? q : p, high = i & 1 ? s : r;
+            return i & 2 ? high : low;
+        }
+    };
+    auto pages_of = [&](int tile, int ids) INLINE {
+        auto at = [&](int i) INLINE {
+            const int id = __builtin_amdgcn_readlane(ids, i);
+            return good(id) && tile * TOKENS + (i << a.page_shift) < length ? (uint64_t)(unsigned)id * page_bytes : (uint64_t)0;
+        };
+        Pages x = {at(0), 0, 0, 0};
+        if (PARTS > 1 && page < TOKENS) {
+            x.b = at(1);
+            if (PARTS > 2) x.c = at(2), x.d = at(3);
+        }
+        return x;
+    };
+    struct Scales {
+        float k, v;      // of this lane's scores and values
+        bool bad;        // the page is none
+    };
+    u32x4 coming[PER];      // keys or values of a tile on their way
+    auto ask_keys = [&](int tile, const Pages& x) INLINE {
 #pragma unroll
-        for (int t = 0; t < SUB; ++t) {
-            const char* kr = kp + t * 4 * D * (EIGHT ? 1 : 2);
+        for (int j = 0; j < PER; ++j)
+            coming[j] = *reinterpret_cast<const u32x4*>(kbase + x[key_chunk(j).part] + (tile * TOKENS & (page - 1)) * (D * SIZE) + key_chunk(j).from);
+    };
+    auto ask_values = [&](int tile, const Pages& x) INLINE {
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            coming[j] = *reinterpret_cast<const u32x4*>(vbase + x[value_chunk(j).part] + (tile * TOKENS & (page - 1)) * SIZE + value_chunk(j).from);
+    };
+    auto put_keys = [&](char* to) INLINE {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) *reinterpret_cast<u32x4*>(to + key_chunk(j).to) = coming[j];
+    };
+    // Nothing of the values behind the sequence's end: those slots hold anything, NaN too.
+    auto put_values = [&](char* to, int tile) INLINE {
+        if ((tile + 1) * TOKENS > length) {
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                const int keep = length - tile * TOKENS - value_chunk(j).token;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int in = min(4, max(0, keep * SIZE - 4 * w));     // bytes of this word
+                    coming[j][w] &= in == 4 ? 0xFFFFFFFFu : (1u << 8 * in) - 1u;
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < PER; ++j) *reinterpret_cast<u32x4*>(to + value_chunk(j).to) = coming[j];
+    };
+    const float *const k_scale = a.cache.k_scale + h, *const v_scale = a.cache.v_scale + h;
+    const int own_part = g * CH >> a.page_shift;
+    auto ask_scales = [&](int tile, int ids) INLINE {      // a lane group's scores are those of its values' tokens
+        int id = __builtin_amdgcn_readlane(ids, 0);
+        if (PARTS > 1 && page < TOKENS) {
+#pragma unroll
+            for (int i = 1; i < PARTS; ++i) {
+                const int other = __builtin_amdgcn_readlane(ids, i);
+                id = own_part == i ? other : id;
+            }
+        }
+        const bool seen_here = tile * TOKENS + g * CH < length;
+        Scales s = {1.f, 1.f, !good(id) && seen_here};
+        if constexpr (EIGHT) {
+            const uint64_t at = (uint64_t)(good(id) && seen_here ? (unsigned)id : 0u) * (unsigned)heads;
+            s.k = k_scale[at];
+            s.v = v_scale[at];
+        }
+        return s;
+    };
+    auto tile_after = [&](int tile) INLINE { return min(tile + NW, last); };
+    int ids = ask_ids(begin);
+    Scales scales = {1.f, 1.f, false};
+
+    // ---- the sequence's own rows
+    const T* const own_k = static_cast<const T*>(a.k) + b * a.sk.seq + h * a.sk.head;
+    const T* const own_v = static_cast<const T*>(a.v) + b * a.sv.seq + h * a.sv.head;
+    auto parent_of = [&](int i, int* bad) INLINE {      // row of the token before row i
+        if (i == 0) return 0;
+        const int p = a.parent ? a.parent[(int64_t)b * a.M + i - 1] : i - 2;
+        if (p >= -1 && p < i - 1) return p + 1;
+        *bad = 1;
+        return 0;
+    };
+    // Own rows on their way to LDS, 8 elements to a thread: keys in the order of the product's rows, values turned over with those that are not
+    // finite taken out.  Neighbouring threads have neighbouring elements of a key, and the same elements of neighbouring values: what
+    // they write then lies next to each other.
+    constexpr int OWN = TOKENS * (D / 8), OWN_PER = (OWN + NT - 1) / NT;
+    struct Taken {
+        Operand k[OWN_PER], v[OWN_PER];
+    };
+    auto take = [&](int base, bool wide) INLINE {
+        Taken t;
+#pragma unroll
+        for (int n = 0; n < OWN_PER; ++n) {
+            const int e = min((int)threadIdx.x + n * NT, OWN - 1);
+            t.k[n] = load8(own_k + min(base + e / (D / 8), rows_of - 1) * a.sk.row + e % (D / 8) * 8, wide);
+            t.v[n] = load8(own_v + min(base + e % TOKENS, rows_of - 1) * a.sv.row + e / TOKENS * 8, wide);
+        }
+        return t;
+    };
+    auto stage = [&](const Taken& t, int base) INLINE {      // returns whether a value is not finite
+        bool odd = false;
+#pragma unroll
+        for (int n = 0; n < OWN_PER; ++n) {
+            const int e = min((int)threadIdx.x + n * NT, OWN - 1), i = e % TOKENS, d = e / TOKENS * 8;
+            *reinterpret_cast<Operand*>(own_keys + Tokens::row_of(e / (D / 8)) * Lds::OWN_KROW + e % (D / 8) * 8 * (int)sizeof(T)) = t.k[n];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float x = base + i < rows_of ? get(t.v[n], j) : 0.f;
+                const bool fine = fabsf(x) < __builtin_huge_valf();
+                odd |= !fine;
+                staged[(d + j) * ROW + i] = (T)(fine ? x : 0.f);
+            }
+        }
+        return odd;
+    };
+    Taken taken;
+    const int i = threadIdx.x;
+    int bad = absent, up = 0;
+    if (has_tree) {
+        taken = a.wide ? take(0, true) : take(0, false);
+        if (i < rows_of) up = parent_of(i, &bad);
+    }
+    Pages at = {0, 0, 0, 0};
+    if (begin < end) {
+        at = pages_of(begin, ids);
+        scales = ask_scales(begin, ids);
+        ids = ask_ids(tile_after(begin));
+        ask_keys(begin, at);
+    }
+    // Ancestors of every row, itself included, as bits: doubling along the parents
+    bool odd = false;
+    if (has_tree) {
+        odd = stage(taken, 0);
+        if (rows_of <= WAVE) {      // one wavefront, a row to a lane
+            if (wave == 0) {
+                unsigned lo = i < 32 ? 1u << i : 0u, hi = i < 32 ? 0u : 1u << (i - 32);
+                while (__any(up != 0)) {
+                    lo |= __shfl(lo, up);
+                    hi |= __shfl(hi, up);
+                    bad |= __shfl(bad, up);
+                    up = __shfl(up, up);
+                }
+                if (i < rows_of) {
+                    seen[i * words] = lo | 1u;
+                    if (words > 1) seen[i * words + 1] = hi;
+                }
+            }
+        } else {
+            if (i < rows_of) {
+                jump[i] = up;
+                lost[i] = bad;
+                for (int w = 0; w < words; ++w) seen[i * words + w] = w == i / 32 ? 1u << i % 32 : 0u;
+            }
+            __syncthreads();
+            for (int more = 1; more;) {
+                unsigned got[MOST_ROWS / 32];
+                int above = 0;
+                if (i < rows_of) {
+                    above = jump[i];
+#pragma unroll
+                    for (int w = 0; w < MOST_ROWS / 32; ++w)
+                        if (w < words) got[w] = seen[above * words + w];
+                    bad = lost[above];
+                    up = jump[above];
+                }
+                more = __syncthreads_or(above != 0);
+                if (i < rows_of) {
+#pragma unroll
+                    for (int w = 0; w < MOST_ROWS / 32; ++w)
+                        if (w < words) seen[i * words + w] |= got[w];
+                    lost[i] |= bad;
+                    jump[i] = up;
+                }
+                __syncthreads();
+            }
+            if (i < rows_of) bad = lost[i];
+        }
+        const uint64_t alive = __ballot(i < rows_of && !bad);
+        if (lane < 2 && 2 * wave + lane < words) present[2 * wave + lane] = (unsigned)(alive >> 32 * lane);
+        odd = __syncthreads_or(odd);
+    }
+
+    // ---- cached tokens, a half of a tile (8 tokens of every lane group) at a time
+    f32x4 s[QT][2];
+    Operand p[QT];
+    auto scores = [&](const char* keys, int half) INLINE {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const char* row = keys + ((2 * half + t) * 16 + col) * Tokens::KROW;
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt) s[qt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
             if constexpr (EIGHT) {
 #pragma unroll
                 for (int j = 0; j < D / 64; ++j) {
-                    const u32x4 w = *reinterpret_cast<const u32x4*>(kr + j * 64 + g * 16);
+                    const u32x4 w = *reinterpret_cast<const u32x4*>(row + j * 64 + g * 16);
+                    const Operand k = from_e4m3<T>(w[0], w[1]), l = from_e4m3<T>(w[2], w[3]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x.k[t][4 * j + i] = w[i];
+                    for (int qt = 0; qt < QT; ++qt) s[qt][t] = mma(k, mine.q[qt][2 * j], s[qt][t]);
+#pragma unroll
+                    for (int qt = 0; qt < QT; ++qt) s[qt][t] = mma(l, mine.q[qt][2 * j + 1], s[qt][t]);
                 }
                 if constexpr (D % 64 != 0) {
-                    const u32x2 w = *reinterpret_cast<const u32x2*>(kr + D / 64 * 64 + g * 8);
-                    x.k[t][D / 64 * 4] = w[0];
-                    x.k[t][D / 64 * 4 + 1] = w[1];
+                    const u32x2 w = *reinterpret_cast<const u32x2*>(row + D / 64 * 64 + g * 8);
+                    const Operand k = from_e4m3<T>(w[0], w[1]);
+#pragma unroll
+                    for (int qt = 0; qt < QT; ++qt) s[qt][t] = mma(k, mine.q[qt][STEPS - 1], s[qt][t]);
                 }
             } else {
 #pragma unroll
                 for (int j = 0; j < STEPS; ++j) {
-                    const u32x4 w = *reinterpret_cast<const u32x4*>(kr + j * 64 + g * 16);
+                    const Operand k = from_bf16<T>(*reinterpret_cast<const u32x4*>(row + j * 64 + g * 16));
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x.k[t][4 * j + i] = w[i];
+                    for (int qt = 0; qt < QT; ++qt) s[qt][t] = mma(k, mine.q[qt][j], s[qt][t]);
                 }
             }
         }
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-            x.v[dt] = *reinterpret_cast<const u32x4*>(vp + (int64_t)(dt * 16 + col) * page * (EIGHT ? 1 : 2));
-        x.f = a.scale;
-        x.vs = 1.f;
-        if constexpr (EIGHT) {      // lane group g's scores are those of its values' tokens
-            x.f *= a.cache.k_scale[(int64_t)vpage * heads + h];
-            x.vs = a.cache.v_scale[(int64_t)vpage * heads + h];
-        }
-        if (!good_v) x.f = __builtin_nanf("");      // what a bad page should have held is not known: the rows become NaN
     };
-
-    Tokens now, next;
-    PageIds ids = {0, 0};
-    if (begin < end) {
-        bring(begin, pages_of(begin), now);
-        if (begin + NW < end) ids = pages_of(begin + NW);
-    }
+    auto outputs = [&](const char* values, int half, float two) INLINE {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+            const char* at = values + (dt * 16 + col) * Tokens::VROW + g * 16;
+            Operand v;
+            if constexpr (EIGHT) {
+                const u32x2 w = *reinterpret_cast<const u32x2*>(at + half * 8);
+                v = from_e4m3<T>(w[0], w[1], two);
+            } else {
+                v = from_bf16<T>(*reinterpret_cast<const u32x4*>(at));
+            }
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt) mine.o[qt][dt] = mma(v, p[qt], mine.o[qt][dt]);
+        }
+    };
+    char* const place = shared + wave * Lds::TILE;
     for (int tile = begin; tile < end; tile += NW) {
-        if (tile + NW < end) {
-            bring(tile + NW, ids, next);
-            if (tile + 2 * NW < end) ids = pages_of(tile + 2 * NW);
+        float f = a.scale * scales.k, vs = scales.v, two = 1.f;
+        f = f < FLT_MIN ? FLT_MIN : f;                   // -inf * f stays -inf
+        if (scales.bad) f = __builtin_nanf("");          // what the page should have held is not known: the rows become NaN
+        if constexpr (EIGHT && sizeof(T) == 2) {         // the scale's power of two goes to the values as they are converted
+            two = __uint_as_float(__float_as_uint(vs) & 0x7F800000u);
+            vs = __uint_as_float((__float_as_uint(vs) & 0x7FFFFFu) | 0x3F800000u);
         }
-        const bool masked = (tile + 1) * TOKENS > length;
-        unsigned vis[QT];
-        if (masked) {
-            const int keep = min(CH, max(0, length - tile * TOKENS - g * CH));
+        const int keep = length - tile * TOKENS - g * CH;
+        if (keep <= 0) f = vs = two = 1.f;
+        // No branch around a load: where two ways meet, the compiler's wait is the longer of theirs.  The last round asks for its own
+        // tile again.
+        wave_sync();
+        put_keys(place);
+        wave_sync();
+        ask_values(tile, at);
+        Operand weights[HALVES][QT];
 #pragma unroll
-            for (int qt = 0; qt < QT; ++qt) vis[qt] = (1u << keep) - 1u;
-            now.cut_values(keep);
-            if (keep == 0) now.f = 0.f, now.vs = 0.f;
-        } else {
+        for (int half = 0; half < HALVES; ++half) {
+            scores(place, half);
+            if ((tile + 1) * TOKENS > length) {
 #pragma unroll
-            for (int qt = 0; qt < QT; ++qt) vis[qt] = ~0u;
-        }
-        f32x4 s[QT][SUB];
+                for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
-        for (int t = 0; t < SUB; ++t) {
-#pragma unroll
-            for (int qt = 0; qt < QT; ++qt) s[qt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < STEPS; ++j) {
-                const Operand k = now.template key<T>(t, j);
-#pragma unroll
-                for (int qt = 0; qt < QT; ++qt) s[qt][t] = mma(k, q[qt][j], s[qt][t]);
+                    for (int j = 0; j < 8; ++j)
+                        if (8 * half + j >= keep) s[qt][j / 4][j % 4] = neg_inf_f();
             }
+            mine.weigh(s, f, vs, weights[half]);
         }
-        Operand p[QT][CH / 8];
-        if (masked) weigh(s, now.f, now.vs, vis, true, p);
-        else weigh(s, now.f, now.vs, vis, false, p);
+        wave_sync();
+        put_values(place, tile);
+        wave_sync();
+        const int to = tile_after(tile);
+        at = pages_of(to, ids);
+        scales = ask_scales(to, ids);
+        ids = ask_ids(tile_after(to));
+        ask_keys(to, at);
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
+        for (int half = 0; half < HALVES; ++half) {
 #pragma unroll
-            for (int i = 0; i < CH / 8; ++i) {
-                const Operand v = now.template value<T>(dt, i);
-#pragma unroll
-                for (int qt = 0; qt < QT; ++qt) o[qt][dt] = mma(v, p[qt][i], o[qt][dt]);
-            }
-        now = next;
+            for (int qt = 0; qt < QT; ++qt) p[qt] = weights[half][qt];
+            outputs(place, half, two);
+        }
     }
 
-    // ---- the sequence's own rows, from the last wavefront on: it has the fewest cached tiles
+    // ---- the sequence's own rows, a half of what is staged to a wavefront, from the last on: it has the fewest cached tiles
     bool gone[QT];
 #pragma unroll
-    for (int qt = 0; qt < QT; ++qt) gone[qt] = false;
-    if (has_tree) {
+    for (int qt = 0; qt < QT; ++qt) gone[qt] = has_tree && !(present[node[qt] >> 5] >> (node[qt] & 31) & 1);
+    for (int base = 0, turn = 0; has_tree && base < rows_of; base += TOKENS) {
+        if (base > 0) {
+            taken = a.wide ? take(base, true) : take(base, false);
+            __syncthreads();
+            odd = __syncthreads_or(stage(taken, base));
+        }
+#pragma unroll 1
+        for (int half = 0; half < HALVES; ++half, ++turn) {
+            if (turn % NW != NW - 1 - wave) continue;
+            const int at = base + g * CH + half * 8;      // the first of this lane group's 8
+            unsigned vis[QT];
 #pragma unroll
-        for (int qt = 0; qt < QT; ++qt) gone[qt] = lost[min(first_row + qt * 16 + col, R - 1) / a.group] != 0;
-        const T* kx = static_cast<const T*>(a.k) + b * a.sk.seq + h * a.sk.head;
-        const T* vx = static_cast<const T*>(a.v) + b * a.sv.seq + h * a.sv.head;
-        for (int base = (NW - 1 - wave) * TOKENS; base < rows_of; base += NW * TOKENS) {
-            unsigned vis[QT], there = 0;
+            for (int qt = 0; qt < QT; ++qt)
+                vis[qt] = gone[qt] || at >= rows_of ? 0u : seen[node[qt] * words + (at >> 5)] >> (at & 31);
 #pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                const int i = base + g * CH + c;
-                if (i < rows_of && !lost[i]) there |= 1u << c;
-            }
-#pragma unroll
-            for (int qt = 0; qt < QT; ++qt) {
-                const int node = min(first_row + qt * 16 + col, R - 1) / a.group;
-                vis[qt] = gone[qt] ? 0u : seen[node * WORDS + (base + g * CH) / 32] >> (g * CH) % 32 & there;
-            }
-            f32x4 s[QT][SUB];
-#pragma unroll
-            for (int t = 0; t < SUB; ++t) {
-                const int i = min(base + col / 4 * CH + 4 * t + col % 4, rows_of - 1);
+            for (int t = 0; t < 2; ++t) {
+                const char* row = own_keys + ((2 * half + t) * 16 + col) * Lds::OWN_KROW;
 #pragma unroll
                 for (int qt = 0; qt < QT; ++qt) s[qt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int j = 0; j < STEPS; ++j) {
-                    const Operand k = load8(kx + i * a.sk.row + Tokens::element(j, g), a.wide);
+                    const Operand k = *reinterpret_cast<const Operand*>(row + Tokens::element(j, g) * (int)sizeof(T));
 #pragma unroll
-                    for (int qt = 0; qt < QT; ++qt) s[qt][t] = mma(k, q[qt][j], s[qt][t]);
+                    for (int qt = 0; qt < QT; ++qt) s[qt][t] = mma(k, mine.q[qt][j], s[qt][t]);
                 }
             }
-            Operand p[QT][CH / 8];
-            weigh(s, a.scale, 1.f, vis, true, p);
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
+            for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
-                for (int i = 0; i < CH / 8; ++i) {
-                    Operand v, odd;
-                    bool any_odd = false;
+                for (int j = 0; j < 8; ++j)
+                    if (!(vis[qt] >> j & 1)) s[qt][j / 4][j % 4] = neg_inf_f();
+            mine.weigh(s, a.scale < FLT_MIN ? FLT_MIN : a.scale, 1.f, p);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                const Operand v = load8(staged + (dt * 16 + col) * ROW + g * CH + half * 8, true);
+#pragma unroll
+                for (int qt = 0; qt < QT; ++qt) mine.o[qt][dt] = mma(v, p[qt], mine.o[qt][dt]);
+            }
+            if (odd) {
+                // A value that is not finite may touch the rows that see it alone, and 0 * NaN is NaN: such values have been taken
+                // out, and here the rows that see one become NaN.
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    Operand what;
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
-                        const int j = base + g * CH + i * 8 + c;
-                        float x = there >> (8 * i + c) & 1 ? (float)vx[j * a.sv.row + dt * 16 + col] : 0.f;
-                        const bool fine = fabsf(x) < __builtin_huge_valf();
-                        any_odd |= !fine;
-                        set(odd, c, fine ? 0.f : 1.f);
-                        set(v, c, fine ? x : 0.f);
+                        const float x = at + c < rows_of ? (float)own_v[(at + c) * a.sv.row + dt * 16 + col] : 0.f;
+                        set(what, c, fabsf(x) < __builtin_huge_valf() ? 0.f : 1.f);
                     }
 #pragma unroll
-                    for (int qt = 0; qt < QT; ++qt) o[qt][dt] = mma(v, p[qt][i], o[qt][dt]);
-                    if (__any(any_odd)) {
-                        // A value that is not finite may touch the rows that see it alone, and 0 * NaN is NaN: such values are taken
-                        // out, and the rows that see one become NaN.
+                    for (int qt = 0; qt < QT; ++qt) {
+                        Operand sees;
 #pragma unroll
-                        for (int qt = 0; qt < QT; ++qt) {
-                            Operand sees;
+                        for (int c = 0; c < 8; ++c) set(sees, c, vis[qt] >> c & 1 ? 1.f : 0.f);
+                        const f32x4 hit = mma(what, sees, f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-                            for (int c = 0; c < 8; ++c) set(sees, c, vis[qt] >> (8 * i + c) & 1 ? 1.f : 0.f);
-                            const f32x4 hit = mma(odd, sees, f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                if (hit[r] > 0.f) o[qt][dt][r] = __builtin_nanf("");
-                        }
+                        for (int r = 0; r < 4; ++r)
+                            if (hit[r] > 0.f) mine.o[qt][dt][r] = __builtin_nanf("");
                     }
                 }
+            }
         }
     }
 
-    // ---- join of the four wavefronts
+    // ---- the wavefronts' parts, each [rows][D + 4], through LDS: 4 elements of a row to a thread
+    constexpr int PART = Lds::PART, ROWS = 16 * QT;
+    float* const joined = reinterpret_cast<float*>(shared);
+    __syncthreads();      // nobody reads tiles and own rows any more
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
-        l[qt] = over_groups_sum(l[qt]);
-        if (too_long && has_tree) l[qt] = __builtin_nanf("");
-        // a row that is not there: no weight, and none of other parts' either
-        if (gone[qt]) m[qt] = __builtin_huge_valf(), l[qt] = 0.f;
+        const float l = mine.sum(qt);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+            *reinterpret_cast<f32x4*>(&joined[wave * PART + (qt * 16 + col) * (D + 4) + dt * 16 + g * 4]) = mine.o[qt][dt];
         if (g == 0) {
-            wave_m[wave][qt * 16 + col] = m[qt];
-            wave_l[wave][qt * 16 + col] = l[qt];
+            // a row that is not there: no weight, and none of other parts' either
+            wave_m[wave][qt * 16 + col] = gone[qt] ? __builtin_huge_valf() : mine.m[qt];
+            wave_l[wave][qt * 16 + col] = gone[qt] ? 0.f : too_long && has_tree ? __builtin_nanf("") : l;
         }
     }
-    __syncthreads();      // and nobody reads the ancestors any more
+    __syncthreads();
+    const int64_t rows_all = (int64_t)a.B * heads * R;
+    constexpr int UNITS = ROWS * (D / 4);
 #pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-        const int i = qt * 16 + col;
-        const float top = fmaxf(fmaxf(wave_m[0][i], wave_m[1][i]), fmaxf(wave_m[2][i], wave_m[3][i]));
-        const float by = gone[qt] ? 0.f : m[qt] == top ? 1.f : __builtin_amdgcn_exp2f(m[qt] - top);
+    for (int n = 0; n < (UNITS + NT - 1) / NT; ++n) {
+        const int e = threadIdx.x + n * NT, rr = e / (D / 4), d = e % (D / 4) * 4, row = first_row + rr;
+        if (e >= UNITS || row >= R) continue;
+        float m[NW], high = neg_inf_f(), all = 0.f;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-            const f32x4 x = gone[qt] ? f32x4{0.f, 0.f, 0.f, 0.f} : o[qt][dt] * by;
-            *reinterpret_cast<f32x4*>(&shared[wave * RED + col * (D + 4) + dt * 16 + g * 4]) = x;
+        for (int w = 0; w < NW; ++w) {
+            m[w] = wave_m[w][rr];
+            high = fmaxf(high, m[w]);
         }
-        __syncthreads();
-        for (int e = threadIdx.x; e < 16 * (D / 4); e += NT) {
-            const int rr = e / (D / 4), d = e % (D / 4) * 4, row = first_row + qt * 16 + rr;
-            if (row >= R) continue;
-            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-            float all = 0.f, high = neg_inf_f();
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < NW; ++w) high = fmaxf(high, wave_m[w][qt * 16 + rr]);
+        for (int w = 0; w < NW; ++w) {
+            const float by = m[w] == high ? 1.f : __builtin_amdgcn_exp2f(m[w] - high);
+            sum += by * *reinterpret_cast<const f32x4*>(&joined[w * PART + rr * (D + 4) + d]);
+            all += by * wave_l[w][rr];
+        }
+        const bool none = all == 0.f;       // nothing seen with a weight, or no row
+        if (a.splits == 1) {
+            const int of = a.by_group.of(row), head = h * a.group + row - of * a.group;
+            typedef typename Vec<T, 4>::type Four;
+            const float per_all = 1.f / all;
+            Four four;
 #pragma unroll
-            for (int w = 0; w < NW; ++w) {
-                sum += *reinterpret_cast<const f32x4*>(&shared[w * RED + rr * (D + 4) + d]);
-                const float mw = wave_m[w][qt * 16 + rr];
-                all += wave_l[w][qt * 16 + rr] * (mw == high ? 1.f : __builtin_amdgcn_exp2f(mw - high));
-            }
-            if (a.splits == 1) {
-                const int node = row / a.group, head = h * a.group + row % a.group;
-                T* out = static_cast<T*>(a.out) + (((int64_t)b * rows_of + node) * a.q_heads + head) * D + d;
-                const float per_all = 1.f / all;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) out[j] = (T)(all == 0.f ? 0.f : sum[j] * per_all);
-            } else {
-                const int64_t rows_all = (int64_t)a.B * heads * R, at = split * rows_all + (int64_t)bh * R + row;
-                *reinterpret_cast<f32x4*>(a.part + at * D + d) = sum;
-                if (d == 0) {
-                    a.part[a.splits * rows_all * D + at] = high;
-                    a.part[a.splits * rows_all * (D + 1) + at] = all;
-                }
+            for (int j = 0; j < 4; ++j) four[j] = (T)(none ? 0.f : sum[j] * per_all);
+            *reinterpret_cast<Four*>(static_cast<T*>(a.out) + (((int64_t)b * rows_of + of) * a.q_heads + head) * D + d) = four;
+        } else {
+            const int64_t at = split * rows_all + (int64_t)bh * R + row;
+            *reinterpret_cast<f32x4*>(a.part + at * D + d) = none ? f32x4{0.f, 0.f, 0.f, 0.f} : sum;
+            if (d == 0) {
+                a.part[a.splits * rows_all * D + at] = high;
+                a.part[a.splits * rows_all * (D + 1) + at] = all;
             }
         }
-        __syncthreads();
     }
 }
 
@@ -530,25 +774,29 @@ __global__ __launch_bounds__(NT) void attend_join_kernel(AttendArgs a) {
 AttendPlan plan_attend(int dtype, int B, int M, int q_heads, const lantern_cache& c, int width) {
     AttendPlan p;
     const int64_t R = (int64_t)(M + 1) * (q_heads / c.heads);
-    // fp32 operands take twice the registers: two tiles of rows
-    const int most = dtype == LANTERN_F32 ? 2 : 4;
-    p.query_tiles = R <= 16 ? 1 : R <= 32 || most == 2 ? 2 : 4;
-    p.row_tiles = (int)((R + 16 * p.query_tiles - 1) / (16 * p.query_tiles));
-    // Workgroups for twice the 256 CUs, as long as each wavefront has two tiles of tokens.
+    // Tiles of 16 rows that a wavefront takes together: each conversion of a tile of tokens serves all of them.  Four (D <= 64, 246 registers)
+    // are no faster where they have all their use: 64 trees of 61 rows 55.1 us against 53.8 with two, one tree 14.8 against 11.3.
+    p.row_group = R <= 16 ? 1 : 2;
+    p.row_tiles = (int)((R + 16 * p.row_group - 1) / (16 * p.row_group));
+    // Workgroups for four times the 256 CUs, as long as each wavefront has two tiles of tokens.
     const int64_t groups = (int64_t)B * c.heads * p.row_tiles, tokens = (int64_t)width * c.page_tokens;
     const int64_t tile = c.dtype == LANTERN_E4M3 ? 64 : 32;
+    // (tiles * splits under 2^31: a table holds 2^30 tokens at most, 2^25 tiles, and parts are 32 or fewer)
     const int64_t useful = std::max<int64_t>(1, tokens / (tile * NW * 2));
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({64, useful, 512 / std::max<int64_t>(1, groups)}));
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({32, useful, 1024 / std::max<int64_t>(1, groups)}));
     p.workspace = p.splits == 1 ? 0 : (size_t)p.splits * B * c.heads * R * (c.D + 2) * sizeof(float);
     return p;
 }
 
 template <typename T, bool EIGHT, int D, int QT>
 static hipError_t launch(const AttendArgs& a, hipStream_t stream) {
+    hipError_t e = allow_lds<attend_trees_kernel<T, EIGHT, D, QT>>(Shared<T, EIGHT, D, QT>::bytes(MOST_ROWS));
+    if (e != hipSuccess) return e;
     const int64_t parts = (int64_t)a.B * a.cache.heads * a.splits;
     const int blocks = (int)((parts + 7) / 8 * 8 * a.row_tiles);
-    hipLaunchKernelGGL((attend_trees_kernel<T, EIGHT, D, QT>), dim3(blocks), dim3(NT), 0, stream, a);
-    hipError_t e = hipGetLastError();
+    const int lds = Shared<T, EIGHT, D, QT>::bytes(a.M + 1);
+    hipLaunchKernelGGL((attend_trees_kernel<T, EIGHT, D, QT>), dim3(blocks), dim3(NT), lds, stream, a);
+    e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     const int64_t threads = (int64_t)a.B * a.q_heads * (a.M + 1) * (D / 4);
     hipLaunchKernelGGL((attend_join_kernel<T>), dim3((unsigned)((threads + NT - 1) / NT)), dim3(NT), 0, stream, a);
@@ -556,28 +804,26 @@ static hipError_t launch(const AttendArgs& a, hipStream_t stream) {
 }
 
 template <typename T, bool EIGHT, int D>
-static hipError_t launch_tiles(const AttendArgs& a, int query_tiles, hipStream_t stream) {
-    if (query_tiles == 1) return launch<T, EIGHT, D, 1>(a, stream);
-    if (query_tiles == 2) return launch<T, EIGHT, D, 2>(a, stream);
-    if constexpr (sizeof(T) == 2) return launch<T, EIGHT, D, 4>(a, stream);
-    return hipErrorInvalidValue;
+static hipError_t launch_rows(const AttendArgs& a, int row_group, hipStream_t stream) {
+    if (row_group == 1) return launch<T, EIGHT, D, 1>(a, stream);
+    return launch<T, EIGHT, D, 2>(a, stream);
 }
 
 template <typename T, bool EIGHT>
-static hipError_t launch_width(const AttendArgs& a, int query_tiles, hipStream_t stream) {
+static hipError_t launch_width(const AttendArgs& a, int row_group, hipStream_t stream) {
     switch (a.cache.D) {
-        case 32: return launch_tiles<T, EIGHT, 32>(a, query_tiles, stream);
-        case 64: return launch_tiles<T, EIGHT, 64>(a, query_tiles, stream);
-        case 96: return launch_tiles<T, EIGHT, 96>(a, query_tiles, stream);
-        case 128: return launch_tiles<T, EIGHT, 128>(a, query_tiles, stream);
+        case 32: return launch_rows<T, EIGHT, 32>(a, row_group, stream);
+        case 64: return launch_rows<T, EIGHT, 64>(a, row_group, stream);
+        case 96: return launch_rows<T, EIGHT, 96>(a, row_group, stream);
+        case 128: return launch_rows<T, EIGHT, 128>(a, row_group, stream);
     }
     return hipErrorInvalidValue;
 }
 
-hipError_t launch_attend_trees(const AttendArgs& a, int dtype, int query_tiles, hipStream_t stream) {
+hipError_t launch_attend_trees(const AttendArgs& a, int dtype, int row_group, hipStream_t stream) {
     const bool eight = a.cache.dtype == LANTERN_E4M3;
-    if (dtype == LANTERN_F32) return eight ? launch_width<float, true>(a, query_tiles, stream) : launch_width<float, false>(a, query_tiles, stream);
-    return eight ? launch_width<bf16, true>(a, query_tiles, stream) : launch_width<bf16, false>(a, query_tiles, stream);
+    if (dtype == LANTERN_F32) return eight ? launch_width<float, true>(a, row_group, stream) : launch_width<float, false>(a, row_group, stream);
+    return eight ? launch_width<bf16, true>(a, row_group, stream) : launch_width<bf16, false>(a, row_group, stream);
 }
 
 hipError_t prepare_attend(int, const lantern_cache&) {

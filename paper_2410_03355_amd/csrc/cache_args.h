@@ -37,29 +37,43 @@ struct AppendArgs {
     int32_t* out_lengths;
 };
 
+// Division by a number that the host knows, for 0 <= n < 2^31.  With 2^(l-1) < d <= 2^l and mul = floor(2^32 (2^l - d) / d) + 1 the
+// quotient is (umulhi(n, mul) + n) >> l.
+struct Divisor {
+    unsigned mul;
+    int shift;
+    Divisor() = default;
+    explicit Divisor(unsigned d) : shift(0) {
+        while ((1ull << shift) < d) ++shift;
+        mul = (unsigned)((((1ull << shift) - d) << 32) / d + 1);
+    }
+    __device__ __forceinline__ int of(int n) const { return (int)((__umulhi((unsigned)n, mul) + (unsigned)n) >> shift); }
+};
+
 struct AttendArgs {
     lantern_cache cache;
     int page_shift;
     const int32_t *table, *lengths, *parent;
     int width, B, M, q_heads, group;   // group: query heads to a key head
-    bool wide;
+    bool wide;              // 16-byte loads of queries, keys and values
     const void *q, *k, *v;
     Strided sq, sk, sv;
     float scale;            // of the scores, times log2(e)
     void* out;              // [B, M + 1, q_heads, D]
     float* part;            // of `splits` parts: their outputs [splits, rows, D], maxima and sums [splits, rows]
     int splits, row_tiles;
+    Divisor by_tiles, by_splits, by_heads, by_group;
 };
 
 struct AttendPlan {
-    int splits, row_tiles, query_tiles;
+    int splits, row_tiles, row_group;
     size_t workspace;
 };
 AttendPlan plan_attend(int dtype, int B, int M, int q_heads, const lantern_cache& c, int width);
 
 hipError_t launch_rotate_axes(const RotateArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_append_cache(const AppendArgs& a, int dtype, hipStream_t stream);
-hipError_t launch_attend_trees(const AttendArgs& a, int dtype, int query_tiles, hipStream_t stream);
+hipError_t launch_attend_trees(const AttendArgs& a, int dtype, int row_group, hipStream_t stream);
 hipError_t prepare_rotate(int dtype);
 hipError_t prepare_append(int dtype, const lantern_cache& c);
 hipError_t prepare_attend(int dtype, const lantern_cache& c);

@@ -98,7 +98,8 @@ def ancestors(parent, T):
 def attend(q, k, v, parent, cache, table, lengths, scale=None):
     """(out, bound on a kernel's error) [B, T, heads, D], fp64.  The bound: a score's exponent is off by the fp32 sum over D
     terms, and by two roundings of its scale; exp2 by 2^-22; the sums over n weights by n half steps each; bf16 rounds every
-    weight by 2^-8 for the product alone; then the output's rounding."""
+    weight w by 2^-8 of it: with w' in both sums, o' - o = sum (w' - w)(v - o) / sum w', at most 2^-8 sum p |v - o|; then the output's
+    rounding."""
     dtype = q.dtype
     half = HALF[dtype]
     B, T, Hq, D = q.shape
@@ -131,9 +132,10 @@ def attend(q, k, v, parent, cache, table, lengths, scale=None):
                 out[b, i, h * G:(h + 1) * G] = o
                 reach = (qq.abs() @ kk.abs().t() * scale).amax(-1, keepdim=True)
                 much = 2 * 2.0 ** -24 * (D + 8) * reach + 2 * 2.0 ** -22 + 2 * 2.0 ** -24 * (len(kk) + 8)
+                room = much * (p @ vv.abs()) + half * o.abs() + 1e-37
                 if dtype == torch.bfloat16:
-                    much = much + 2.0 ** -8
-                bound[b, i, h * G:(h + 1) * G] = much * (p @ vv.abs()) + half * o.abs() + 1e-37
+                    room = room + 2.0 ** -8 * (p @ vv.abs() + o.abs())
+                bound[b, i, h * G:(h + 1) * G] = room
     return out, bound
 
 
