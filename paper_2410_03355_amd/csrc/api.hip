@@ -449,7 +449,7 @@ int attend_plan(lantern_dtype dtype, int B, int M, int q_heads, const lantern_ca
     const int64_t group = q_heads / cache->heads;
     if (group * (M + 1) > INT_MAX / 2 || (int64_t)B * q_heads > INT_MAX / (M + 1)) return LANTERN_E_SHAPE;
     *plan = lantern::plan_attend(dtype, B, M, q_heads, *cache, width);
-    return ((int64_t)B * cache->heads * plan->splits + 8) * plan->row_tiles > INT_MAX ? LANTERN_E_SHAPE : LANTERN_OK;
+    return ((int64_t)plan->parts * cache->heads + 8) * plan->row_tiles > INT_MAX ? LANTERN_E_SHAPE : LANTERN_OK;
 }
 
 }  // namespace
@@ -571,10 +571,10 @@ int lantern_attend_trees(const void* q, const int64_t* q_strides, const void* k,
     a.scale = (float)((double)scale * 1.4426950408889634074);
     a.out = out;
     a.part = static_cast<float*>(workspace);
-    a.splits = plan.splits;
+    a.parts = plan.parts;
+    a.per_part = plan.parts > B ? (1.0 + 1e-12) / (plan.parts - B) : 0.0;
     a.row_tiles = plan.row_tiles;
     a.by_tiles = lantern::Divisor(plan.row_tiles);
-    a.by_splits = lantern::Divisor(plan.splits);
     a.by_heads = lantern::Divisor(cache->heads);
     a.by_group = lantern::Divisor(a.group);
     const hipError_t e = lantern::launch_attend_trees(a, dtype, plan.row_group, static_cast<hipStream_t>(hip_stream));

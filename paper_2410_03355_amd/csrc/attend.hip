@@ -243,6 +243,31 @@ struct Shared {
     }
 };
 
+// Parts of the B sequences where there are `parts` > B: all are of as many tiles of tokens, the last of a sequence of what is left, and
+// a sequence has one at least.  With tiles T_b and size = T / (parts - B), sum ceil(T_b / size) <= parts.  Every wavefront finds its
+// part from the lengths by itself.
+struct Parts {
+    int size;      // tiles
+    __device__ __forceinline__ static int tiles_of(const AttendArgs& a, int b, int tokens) {
+        const int n = b < a.B ? a.lengths[b] : 0;
+        return n < 0 || (int64_t)n > (int64_t)a.width << a.page_shift ? 0 : (n + tokens - 1) / tokens;
+    }
+    __device__ __forceinline__ Parts(const AttendArgs& a, int tokens) {
+        const int lane = threadIdx.x & (WAVE - 1);
+        int low = 0, high = 0;      // two sums: up to 512 sequences of 2^25 tiles
+        for (int b = lane; b < a.B; b += WAVE) {
+            const int t = tiles_of(a, b, tokens);
+            low += t & 0xFFFF;
+            high += t >> 16;
+        }
+        low = __builtin_amdgcn_readlane(wave_scan_i<OpSum>(low, 0), WAVE - 1);
+        high = __builtin_amdgcn_readlane(wave_scan_i<OpSum>(high, 0), WAVE - 1);
+        const int most = (int)(((double)high * 65536.0 + (double)low) * a.per_part) + 1;      // per_part: 1 / (parts - B), a little more
+        size = (most + NW - 1) / NW * NW;
+    }
+    __device__ __forceinline__ int count(int tiles) const { return tiles <= size ? 1 : (int)((unsigned)(tiles + size - 1) / (unsigned)size); }
+};
+
 // Four wavefronts take the same QT * 16 rows, each through every fourth tile of a sequence's cached tokens.
 template <typename T, bool EIGHT, int D, int QT>
 __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_trees_kernel(AttendArgs a) {
@@ -265,13 +290,36 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
     int *const jump = reinterpret_cast<int*>(present + words), *const lost = jump + rows_of;
     // The row tiles of one part of a sequence and head read the same tokens: they get numbers 8 apart, which one XCD serves.
     const int chunk = a.by_tiles.of(blockIdx.x >> 3);
-    const int part = chunk * 8 + (int)(blockIdx.x & 7), first_row = ((int)(blockIdx.x >> 3) - chunk * a.row_tiles) * 16 * QT;
-    if (part >= a.B * heads * a.splits) return;
-    const int bh = a.by_splits.of(part), split = part - bh * a.splits, b = a.by_heads.of(bh), h = bh - b * heads;
+    const int item = chunk * 8 + (int)(blockIdx.x & 7), first_row = ((int)(blockIdx.x >> 3) - chunk * a.row_tiles) * 16 * QT;
+    const int part = a.by_heads.of(item), h = item - part * heads;
+    if (part >= a.parts) return;
+    int b = part, nth = 0, size = INT_MAX;      // the sequence, its part, and how many tiles that has
+    bool whole = true;
+    if (a.parts > a.B) {
+        const Parts parts(a, TOKENS);
+        size = parts.size;
+        b = -1;
+        for (int base = 0, before = 0; base < a.B; base += WAVE) {
+            const int n = base + lane < a.B ? parts.count(Parts::tiles_of(a, base + lane, TOKENS)) : 0;
+            const int upto = before + wave_scan_i<OpSum>(n, 0);
+            const uint64_t mine = __ballot(part >= upto - n && part < upto);
+            if (mine) {
+                const int at = __ffsll((long long)mine) - 1;
+                b = base + at;
+                nth = part - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(n, at));
+                whole = __builtin_amdgcn_readlane(n, at) == 1;
+                break;
+            }
+            before = __builtin_amdgcn_readlane(upto, WAVE - 1);
+        }
+        if (b < 0) return;      // fewer parts than there is room for
+    }
     const int told = a.lengths[b], page = 1 << a.page_shift;
     const bool absent = told < 0, too_long = (int64_t)told > (int64_t)a.width << a.page_shift;
     const int length = absent || too_long ? 0 : told;
-    const bool has_tree = split == a.splits - 1;
+    const int tiles = (length + TOKENS - 1) / TOKENS;
+    const int begin = whole ? wave : nth * size + wave, end = whole ? tiles : min(tiles, (nth + 1) * size);
+    const bool has_tree = whole || (nth + 1) * size >= tiles;
 
     // ---- the rows: B of the first product
     Mine mine;
@@ -292,10 +340,6 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
     mine.begin();
 
     // ---- where the cached tokens are
-    const int tiles = (length + TOKENS - 1) / TOKENS;
-    // tiles * splits stays under 2^31 (plan_attend); one part begins at 0 whatever the length
-    const int begin = a.splits == 1 ? wave : a.by_splits.of(tiles * split) + wave;
-    const int end = a.splits == 1 ? tiles : a.by_splits.of(tiles * (split + 1));
     const int last = begin < end ? begin + (end - 1 - begin) / NW * NW : begin;      // this wavefront's last tile
     const int32_t* const table = a.table + (int64_t)b * a.width;
     const unsigned page_bytes = (unsigned)heads * page * D * SIZE;      // 65535 heads at most: under 2^31
@@ -705,7 +749,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
         }
     }
     __syncthreads();
-    const int64_t rows_all = (int64_t)a.B * heads * R;
+    const int64_t rows_all = (int64_t)a.parts * heads * R;
     constexpr int UNITS = ROWS * (D / 4);
 #pragma unroll
     for (int n = 0; n < (UNITS + NT - 1) / NT; ++n) {
@@ -725,7 +769,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
             all += by * wave_l[w][rr];
         }
         const bool none = all == 0.f;       // nothing seen with a weight, or no row
-        if (a.splits == 1) {
+        if (whole) {
             const int of = a.by_group.of(row), head = h * a.group + row - of * a.group;
             typedef typename Vec<T, 4>::type Four;
             const float per_all = 1.f / all;
@@ -734,41 +778,76 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
             for (int j = 0; j < 4; ++j) four[j] = (T)(none ? 0.f : sum[j] * per_all);
             *reinterpret_cast<Four*>(static_cast<T*>(a.out) + (((int64_t)b * rows_of + of) * a.q_heads + head) * D + d) = four;
         } else {
-            const int64_t at = split * rows_all + (int64_t)bh * R + row;
+            const int64_t at = (int64_t)item * R + row;
             *reinterpret_cast<f32x4*>(a.part + at * D + d) = none ? f32x4{0.f, 0.f, 0.f, 0.f} : sum;
             if (d == 0) {
-                a.part[a.splits * rows_all * D + at] = high;
-                a.part[a.splits * rows_all * (D + 1) + at] = all;
+                a.part[rows_all * D + at] = high;
+                a.part[rows_all * (D + 1) + at] = all;
             }
         }
     }
 }
 
-// The parts of a sequence's rows joined: D / 4 threads to a row.
+// The parts of a sequence's rows joined.  A workgroup takes 64 pieces of 4 elements of the rows of one sequence and head, a piece to a lane,
+// and its wavefronts every fourth part.  Sequences of one part have been written already.
 template <typename T>
-__global__ __launch_bounds__(NT) void attend_join_kernel(AttendArgs a) {
-    const int D = a.cache.D, per_row = D / 4, rows_of = a.M + 1, R = rows_of * a.group, heads = a.cache.heads;
-    const int64_t rows_all = (int64_t)a.B * heads * R, at = (int64_t)blockIdx.x * NT + threadIdx.x, row = at / per_row;
-    if (row >= rows_all) return;
-    const int d = (int)(at % per_row) * 4;
-    const float *pm = a.part + a.splits * rows_all * D, *pl = pm + a.splits * rows_all;
-    float high = neg_inf_f();
-    for (int s = 0; s < a.splits; ++s) high = fmaxf(high, pm[s * rows_all + row]);
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    float all = 0.f;
-    bool gone = false;
-#pragma unroll 4
-    for (int s = 0; s < a.splits; ++s) {
-        const float ms = pm[s * rows_all + row], ls = pl[s * rows_all + row], by = ms == high ? 1.f : __builtin_amdgcn_exp2f(ms - high);
-        gone |= ms == __builtin_huge_valf() && ls == 0.f;
-        all += by * ls;
-        sum += by * *reinterpret_cast<const f32x4*>(a.part + (s * rows_all + row) * D + d);
+__global__ __launch_bounds__(NT) void attend_join_kernel(AttendArgs a, int tokens) {
+    __shared__ f32x4 sums[NW][WAVE];
+    __shared__ float highs[NW][WAVE], alls[NW][WAVE];
+    const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), heads = a.cache.heads, D = a.cache.D, rows_of = a.M + 1, R = rows_of * a.group;
+    const int b = blockIdx.x, h = blockIdx.y;
+    const Parts parts(a, tokens);
+    int first = 0, n = 0;
+    for (int base = 0; base <= b; base += WAVE) {
+        const int mine = base + lane < a.B ? parts.count(Parts::tiles_of(a, base + lane, tokens)) : 0;
+        const int upto = wave_scan_i<OpSum>(mine, 0), at = min(b - base, WAVE - 1);
+        n = __builtin_amdgcn_readlane(mine, at);
+        first += __builtin_amdgcn_readlane(upto, at) - (b - base < WAVE ? n : 0);
     }
-    const int r = (int)(row % R), bh = (int)(row / R), node = r / a.group, head = bh % heads * a.group + r % a.group;
-    T* out = static_cast<T*>(a.out) + (((int64_t)(bh / heads) * rows_of + node) * a.q_heads + head) * D + d;
-    const float per_all = 1.f / all;
+    if (n == 1) return;
+    const int64_t rows_all = (int64_t)a.parts * heads * R;
+    const float *const pm = a.part + rows_all * D, *const pl = pm + rows_all;
+    const int per_row = D / 4, units = R * per_row, unit = blockIdx.z * WAVE + lane;
+    const int row = min(unit, units - 1) / per_row, d = min(unit, units - 1) % per_row * 4;
+    float high = neg_inf_f(), all = 0.f;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    bool gone = false;
+    auto take = [&](float m, float l, f32x4 o) INLINE {
+        gone |= m == __builtin_huge_valf() && l == 0.f;
+        const float to = fmaxf(high, m), was = high == to ? 1.f : __builtin_amdgcn_exp2f(high - to), by = m == to ? 1.f : __builtin_amdgcn_exp2f(m - to);
+        high = to;
+        all = all * was + l * by;
+        sum = sum * was + o * by;
+    };
+    constexpr int AHEAD = 4;
+    for (int i = wave; i < n; i += AHEAD * NW) {
+        float m[AHEAD], l[AHEAD];
+        f32x4 o[AHEAD];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) out[j] = (T)(gone || all == 0.f ? 0.f : sum[j] * per_all);
+        for (int j = 0; j < AHEAD; ++j) {      // past the end the last one again, without a weight
+            const int64_t at = ((int64_t)(first + min(i + j * NW, n - 1)) * heads + h) * R + row;
+            m[j] = pm[at];
+            l[j] = pl[at];
+            o[j] = *reinterpret_cast<const f32x4*>(a.part + at * D + d);
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+            if (i + j * NW < n) take(m[j], l[j], o[j]);
+    }
+    highs[wave][lane] = gone ? __builtin_huge_valf() : high;
+    alls[wave][lane] = gone ? 0.f : all;
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave > 0 || unit >= units) return;
+    for (int w = 1; w < NW; ++w) take(highs[w][lane], alls[w][lane], sums[w][lane]);
+    const bool none = gone || all == 0.f;
+    const int node = a.by_group.of(row), head = h * a.group + row - node * a.group;
+    typedef typename Vec<T, 4>::type Four;
+    const float per_all = 1.f / all;
+    Four four;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) four[j] = (T)(none ? 0.f : sum[j] * per_all);
+    *reinterpret_cast<Four*>(static_cast<T*>(a.out) + (((int64_t)b * rows_of + node) * a.q_heads + head) * D + d) = four;
 }
 
 AttendPlan plan_attend(int dtype, int B, int M, int q_heads, const lantern_cache& c, int width) {
@@ -778,13 +857,14 @@ AttendPlan plan_attend(int dtype, int B, int M, int q_heads, const lantern_cache
     // are no faster where they have all their use: 64 trees of 61 rows 55.1 us against 53.8 with two, one tree 14.8 against 11.3.
     p.row_group = R <= 16 ? 1 : 2;
     p.row_tiles = (int)((R + 16 * p.row_group - 1) / (16 * p.row_group));
-    // Workgroups for four times the 256 CUs, as long as each wavefront has two tiles of tokens.
-    const int64_t groups = (int64_t)B * c.heads * p.row_tiles, tokens = (int64_t)width * c.page_tokens;
-    const int64_t tile = c.dtype == LANTERN_E4M3 ? 64 : 32;
-    // (tiles * splits under 2^31: a table holds 2^30 tokens at most, 2^25 tiles, and parts are 32 or fewer)
+    // Where sequences, heads and row tiles make fewer workgroups than fit the 256 CUs at once (two or three to a CU), sequences are cut:
+    // into parts of two tiles to a wavefront at least.
+    const int64_t groups = (int64_t)c.heads * p.row_tiles, tokens = (int64_t)width * c.page_tokens;
+    const int64_t room = dtype == LANTERN_BF16 && c.D <= 64 ? 768 : 512, tile = c.dtype == LANTERN_E4M3 ? 64 : 32;
     const int64_t useful = std::max<int64_t>(1, tokens / (tile * NW * 2));
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({32, useful, 1024 / std::max<int64_t>(1, groups)}));
-    p.workspace = p.splits == 1 ? 0 : (size_t)p.splits * B * c.heads * R * (c.D + 2) * sizeof(float);
+    const int64_t parts = std::min(room / groups, B * useful);
+    p.parts = (int)(parts >= 2 * (int64_t)B ? parts : B);
+    p.workspace = p.parts == B ? 0 : (size_t)p.parts * c.heads * R * (c.D + 2) * sizeof(float);
     return p;
 }
 
@@ -792,14 +872,14 @@ template <typename T, bool EIGHT, int D, int QT>
 static hipError_t launch(const AttendArgs& a, hipStream_t stream) {
     hipError_t e = allow_lds<attend_trees_kernel<T, EIGHT, D, QT>>(Shared<T, EIGHT, D, QT>::bytes(MOST_ROWS));
     if (e != hipSuccess) return e;
-    const int64_t parts = (int64_t)a.B * a.cache.heads * a.splits;
-    const int blocks = (int)((parts + 7) / 8 * 8 * a.row_tiles);
+    const int64_t items = (int64_t)a.parts * a.cache.heads;
+    const int R = (a.M + 1) * a.group;
+    const int blocks = (int)((items + 7) / 8 * 8 * a.row_tiles);
     const int lds = Shared<T, EIGHT, D, QT>::bytes(a.M + 1);
     hipLaunchKernelGGL((attend_trees_kernel<T, EIGHT, D, QT>), dim3(blocks), dim3(NT), lds, stream, a);
     e = hipGetLastError();
-    if (e != hipSuccess || a.splits == 1) return e;
-    const int64_t threads = (int64_t)a.B * a.q_heads * (a.M + 1) * (D / 4);
-    hipLaunchKernelGGL((attend_join_kernel<T>), dim3((unsigned)((threads + NT - 1) / NT)), dim3(NT), 0, stream, a);
+    if (e != hipSuccess || a.parts == a.B) return e;
+    hipLaunchKernelGGL((attend_join_kernel<T>), dim3(a.B, a.cache.heads, (R * (D / 4) + WAVE - 1) / WAVE), dim3(NT), 0, stream, a, (int)Tile<EIGHT, D>::TOKENS);
     return hipGetLastError();
 }
 

@@ -60,13 +60,14 @@ struct AttendArgs {
     Strided sq, sk, sv;
     float scale;            // of the scores, times log2(e)
     void* out;              // [B, M + 1, q_heads, D]
-    float* part;            // of `splits` parts: their outputs [splits, rows, D], maxima and sums [splits, rows]
-    int splits, row_tiles;
-    Divisor by_tiles, by_splits, by_heads, by_group;
+    int parts, row_tiles;   // parts of all sequences, B or more
+    double per_part;        // 1 / (parts - B), a little more
+    float* part;            // where they are more: outputs [parts, heads, rows, D], then maxima and sums [parts, heads, rows]
+    Divisor by_tiles, by_heads, by_group;
 };
 
 struct AttendPlan {
-    int splits, row_tiles, row_group;
+    int parts, row_tiles, row_group;
     size_t workspace;
 };
 AttendPlan plan_attend(int dtype, int B, int M, int q_heads, const lantern_cache& c, int width);
