@@ -801,6 +801,10 @@ def rotate_axes(q, k, positions, freqs, sections, interleaved: bool = False, inv
     each axis, freqs [their sum].  Returns (q, k) turned, new tensors or those of `out` (a pair, which may be q and k
     themselves).  inverse turns back, which is the gradient: it takes the outputs' gradients to the inputs'."""
     lib = load()
+    if out is None and stream is None:
+        got = _marshal.rotate_axes(q, k, positions, freqs, sections, interleaved, inverse)
+        if got is not None:
+            return _checked_status(got, "lantern_rotate_axes")
     ts = [t for t in (q, k) if t is not None]
     for t in ts:
         if t.dim() != 3 or t.shape[0] != q.shape[0] or t.shape[2] != q.shape[2] or t.dtype != q.dtype or (t.shape[2] > 1 and t.stride(2) != 1):
@@ -840,6 +844,10 @@ def append_cache(cache, table, lengths, k, v, positions=None, freqs=None, sectio
     turned by positions [B, T, axes] if given.  Which rows: path [B, T-1] and count [B] as verify_trees returns them (row 0,
     then the accepted candidates), or the first count [B], or all.  Returns the new lengths int32[B] (-2: left as it was)."""
     lib = load()
+    if stream is None:
+        got = _marshal.append_cache(cache, table, lengths, k, v, positions, freqs, sections, interleaved, path, count)
+        if got is not None:
+            return _checked_status(got, "lantern_append_cache")
     c, parts = _cache_args(cache)
     _rows_of_cache(c, k, v)
     B, T = k.shape[:2]
@@ -877,6 +885,10 @@ def attend_trees(q, k, v, parent, cache, table, lengths, scale=None, workspace=N
     tree of parent int32[B*M] (None: every row follows the one before it).  scale: D ** -0.5 unless given.  workspace: a
     uint8 tensor of at least attend_trees_workspace_bytes, or None to allocate one.  Returns out [B, 1 + M, heads, D]."""
     lib = load()
+    if stream is None:
+        got = _marshal.attend_trees(q, k, v, parent, cache, table, lengths, scale, workspace)
+        if got is not None:
+            return _checked_status(got, "lantern_attend_trees")
     c, parts = _cache_args(cache)
     _rows_of_cache(c, k, v)
     B, T = k.shape[:2]

@@ -20,6 +20,7 @@
 
 #include <algorithm>
 #include <climits>
+#include <cmath>
 
 #include "lantern.h"
 
@@ -37,6 +38,10 @@ decltype(&lantern_verify_trees_sequential) c_verify_trees_sequential;
 decltype(&lantern_verify_trees_sequential_workspace_bytes) c_sequential_bytes;
 decltype(&lantern_accept_chains) c_accept_chains;
 decltype(&lantern_accept_trees) c_accept_trees;
+decltype(&lantern_rotate_axes) c_rotate_axes;
+decltype(&lantern_append_cache) c_append_cache;
+decltype(&lantern_attend_trees_workspace_bytes) c_attend_bytes;
+decltype(&lantern_attend_trees) c_attend_trees;
 
 // Interpreter modes see every torch call of the Python functions: with one active those run.
 bool modes_active() {
@@ -356,6 +361,140 @@ PyObject* accept_trees(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     return result(status, len, path, next);
 }
 
+// ---- the calls around a tree step.  Their tensors are all on the current device, or the call is declined.
+
+bool here(const at::Tensor& t) { return t.device().index() == c10::hip::current_device(); }
+const at::Tensor* near(PyObject* o) {
+    const at::Tensor* t = plain(o);
+    return t && here(*t) ? t : nullptr;
+}
+const at::Tensor* near(PyObject* o, at::ScalarType type) {
+    const at::Tensor* t = plain(o, type);
+    return t && here(*t) ? t : nullptr;
+}
+bool heads_type(const at::Tensor& t, lantern_dtype* type) {
+    if (t.scalar_type() == at::kFloat) *type = LANTERN_F32;
+    else if (t.scalar_type() == at::kBFloat16) *type = LANTERN_BF16;
+    else return false;
+    return true;
+}
+// [.., heads, D] with dense heads, `dims` of them, nothing empty.
+const at::Tensor* heads_of(PyObject* o, int dims) {
+    const at::Tensor* t = near(o);
+    if (!t || t->dim() != dims || t->stride(dims - 1) != 1) return nullptr;
+    for (int i = 0; i < dims; ++i)
+        if (t->size(i) < 1 || t->size(i) > INT_MAX) return nullptr;
+    return t;
+}
+bool alike(const at::Tensor& a, const at::Tensor& b) { return a.sizes() == b.sizes() && a.scalar_type() == b.scalar_type(); }
+
+bool cache_of(PyObject* o, lantern_cache* c) {
+    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) return false;
+    const at::Tensor *k = near(PyTuple_GET_ITEM(o, 0)), *v = near(PyTuple_GET_ITEM(o, 1));
+    if (!k || !v || k->dim() != 4 || v->dim() != 4 || !k->is_contiguous() || !v->is_contiguous() || k->scalar_type() != v->scalar_type() ||
+        v->size(0) != k->size(0) || v->size(1) != k->size(1) || v->size(2) != k->size(3) || v->size(3) != k->size(2) || k->size(0) > INT_MAX)
+        return false;
+    *c = {k->data_ptr(), v->data_ptr(), nullptr, nullptr, LANTERN_BF16, (int)k->size(0), (int)k->size(1), (int)k->size(2), (int)k->size(3)};
+    if (k->scalar_type() == at::kBFloat16) return true;
+    const at::Tensor *ks = near(PyTuple_GET_ITEM(o, 2), at::kFloat), *vs = near(PyTuple_GET_ITEM(o, 3), at::kFloat);
+    if (k->scalar_type() != at::kFloat8_e4m3fn || !ks || !vs || ks->sizes() != k->sizes().slice(0, 2) || vs->sizes() != ks->sizes()) return false;
+    c->k_scale = ks->data_ptr<float>();
+    c->v_scale = vs->data_ptr<float>();
+    c->dtype = LANTERN_E4M3;
+    return true;
+}
+// positions [rows, axes], freqs, sections: a tuple of whole numbers
+bool rotation_of(PyObject* pos, PyObject* freqs, PyObject* sections, PyObject* inter, int64_t rows, lantern_rotation* r) {
+    const at::Tensor *p = near(pos, at::kInt), *f = near(freqs, at::kFloat);
+    if (!p || !f || !PyTuple_CheckExact(sections) || !PyBool_Check(inter)) return false;
+    const Py_ssize_t axes = PyTuple_GET_SIZE(sections);
+    if (axes < 1 || axes > LANTERN_MAX_AXES || p->numel() != rows * axes) return false;
+    *r = {p->const_data_ptr<int32_t>(), f->const_data_ptr<float>(), (int)axes, {0, 0, 0, 0}, inter == Py_True};
+    int64_t sum = 0;
+    for (Py_ssize_t i = 0; i < axes; ++i)
+        if (!count(PyTuple_GET_ITEM(sections, i), &r->pairs[i])) return false;
+        else sum += r->pairs[i];
+    return f->numel() == sum;
+}
+bool table_of(PyObject* table, PyObject* lengths, int64_t B, const at::Tensor** t, const at::Tensor** n) {
+    *t = near(table, at::kInt);
+    *n = near(lengths, at::kInt);
+    return *t && *n && (*t)->dim() == 2 && (*t)->size(0) == B && (*t)->size(1) >= 1 && (*t)->size(1) <= INT_MAX && (*n)->numel() == B;
+}
+PyObject* single(PyObject* one) {      // of a tuple of one
+    if (!one || !PyTuple_CheckExact(one)) return one;
+    PyObject* out = PyTuple_GET_ITEM(one, 0);
+    Py_INCREF(out);
+    Py_DECREF(one);
+    return out;
+}
+
+// q, k, positions, freqs, sections, interleaved, inverse
+PyObject* rotate_axes(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    const at::Tensor *q = nullptr, *k = nullptr;
+    lantern_dtype type = LANTERN_F32;
+    lantern_rotation r;
+    ORDINARY(7, (q = heads_of(a[0], 3)) && (k = heads_of(a[1], 3)) && heads_type(*q, &type) && k->scalar_type() == q->scalar_type() &&
+                    k->size(0) == q->size(0) && k->size(2) == q->size(2) && rotation_of(a[2], a[3], a[4], a[5], q->size(0), &r) &&
+                    PyBool_Check(a[6]))
+    at::Tensor oq, ok;
+    int status = 0;
+    RUN(oq = at::empty(q->sizes(), q->options()); ok = at::empty(k->sizes(), k->options());
+        return c_rotate_axes(q->const_data_ptr(), q->strides().data(), (int)q->size(1), k->const_data_ptr(), k->strides().data(), (int)k->size(1),
+                             type, (int)q->size(0), (int)q->size(2), &r, a[6] == Py_True, oq.mutable_data_ptr(), oq.strides().data(),
+                             ok.mutable_data_ptr(), ok.strides().data(), current_stream());)
+    return result(status, oq, ok);
+}
+
+// cache, table, lengths, k, v, positions, freqs, sections, interleaved, path, count
+PyObject* append_cache(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    lantern_cache c;
+    lantern_rotation r;
+    lantern_dtype type = LANTERN_F32;
+    const at::Tensor *table = nullptr, *lengths = nullptr, *k = nullptr, *v = nullptr, *path = nullptr, *some = nullptr;
+    const auto rows = [&] { return k->size(0) * k->size(1); };
+    ORDINARY(11, cache_of(a[0], &c) && (k = heads_of(a[3], 4)) && (v = heads_of(a[4], 4)) && alike(*k, *v) && heads_type(*k, &type) &&
+                     k->size(2) == c.heads && k->size(3) == c.D && table_of(a[1], a[2], k->size(0), &table, &lengths) &&
+                     (a[5] == Py_None || rotation_of(a[5], a[6], a[7], a[8], rows(), &r)) &&
+                     (a[9] == Py_None || ((path = near(a[9], at::kInt)) && path->numel() == rows() - k->size(0) && a[10] != Py_None)) &&
+                     (a[10] == Py_None || ((some = near(a[10], at::kInt)) && some->numel() == k->size(0))))
+    at::Tensor out;
+    int status = 0;
+    RUN(out = at::empty({k->size(0)}, lengths->options());
+        return c_append_cache(&c, table->const_data_ptr<int32_t>(), (int)table->size(1), lengths->const_data_ptr<int32_t>(), (int)k->size(0),
+                              (int)k->size(1), k->const_data_ptr(), k->strides().data(), v->const_data_ptr(), v->strides().data(), type,
+                              a[5] == Py_None ? nullptr : &r, path ? path->const_data_ptr<int32_t>() : nullptr,
+                              some ? some->const_data_ptr<int32_t>() : nullptr, data(out), current_stream());)
+    return single(result(status, out));
+}
+
+// q, k, v, parent, cache, table, lengths, scale, workspace
+PyObject* attend_trees(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    lantern_cache c;
+    lantern_dtype type = LANTERN_F32;
+    const at::Tensor *q = nullptr, *k = nullptr, *v = nullptr, *parent = nullptr, *table = nullptr, *lengths = nullptr, *given = nullptr;
+    float scale = 0.f;
+    ORDINARY(9, (q = heads_of(a[0], 4)) && (k = heads_of(a[1], 4)) && (v = heads_of(a[2], 4)) && alike(*k, *v) && heads_type(*q, &type) &&
+                    q->scalar_type() == k->scalar_type() && q->size(0) == k->size(0) && q->size(1) == k->size(1) && q->size(3) == k->size(3) &&
+                    cache_of(a[4], &c) && k->size(2) == c.heads && k->size(3) == c.D && table_of(a[5], a[6], k->size(0), &table, &lengths) &&
+                    (a[3] == Py_None || ((parent = near(a[3], at::kInt)) && parent->numel() == k->size(0) * (k->size(1) - 1))) &&
+                    (a[7] == Py_None || real(a[7], &scale)) && (a[8] == Py_None || ((given = near(a[8])) && given->is_contiguous())))
+    if (a[7] == Py_None) scale = (float)std::pow((double)c.D, -0.5);
+    at::Tensor out, work;
+    int status = 0;
+    RUN(const int B = (int)k->size(0), M = (int)k->size(1) - 1, heads = (int)q->size(2), width = (int)table->size(1);
+        const size_t need = c_attend_bytes(type, B, M, heads, &c, width);
+        if (given) work = *given;
+        else if (need) work = at::empty({(int64_t)need}, at::TensorOptions().dtype(at::kByte).device(q->device()));
+        out = at::empty({B, M + 1, heads, c.D}, q->options());
+        return c_attend_trees(q->const_data_ptr(), q->strides().data(), k->const_data_ptr(), k->strides().data(), v->const_data_ptr(),
+                              v->strides().data(), type, B, M, heads, parent ? parent->const_data_ptr<int32_t>() : nullptr, &c,
+                              table->const_data_ptr<int32_t>(), width, lengths->const_data_ptr<int32_t>(), scale, out.mutable_data_ptr(),
+                              work.defined() ? work.mutable_data_ptr() : nullptr, work.defined() ? work.numel() * work.element_size() : 0,
+                              current_stream());)
+    return single(result(status, out));
+}
+
 // bind({"lantern_verify": address, ...})
 PyObject* bind(PyObject*, PyObject* table) {
     const auto set = [&](auto& f, const char* name) {
@@ -370,7 +509,9 @@ PyObject* bind(PyObject*, PyObject* table) {
         set(c_verify_trees_greedy, "lantern_verify_trees_greedy") &&
         set(c_verify_trees_sequential, "lantern_verify_trees_sequential") &&
         set(c_sequential_bytes, "lantern_verify_trees_sequential_workspace_bytes") &&
-        set(c_accept_chains, "lantern_accept_chains") && set(c_accept_trees, "lantern_accept_trees"))
+        set(c_accept_chains, "lantern_accept_chains") && set(c_accept_trees, "lantern_accept_trees") &&
+        set(c_rotate_axes, "lantern_rotate_axes") && set(c_append_cache, "lantern_append_cache") &&
+        set(c_attend_bytes, "lantern_attend_trees_workspace_bytes") && set(c_attend_trees, "lantern_attend_trees"))
         Py_RETURN_NONE;
     return nullptr;
 }
@@ -378,7 +519,8 @@ PyObject* bind(PyObject*, PyObject* table) {
 #define FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"bind", bind, METH_O, nullptr}, FAST(verify), FAST(verify_rows), FAST(decide_rows),
                          FAST(verify_greedy), FAST(verify_greedy_rows), FAST(verify_trees), FAST(verify_trees_sequential),
-                         FAST(verify_trees_greedy), FAST(accept_chains), FAST(accept_trees), {nullptr, nullptr, 0, nullptr}};
+                         FAST(verify_trees_greedy), FAST(accept_chains), FAST(accept_trees), FAST(rotate_axes), FAST(append_cache),
+                         FAST(attend_trees), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
