@@ -604,7 +604,7 @@ int lantern_rotate_axes(const void* q, const int64_t* q_strides, int q_heads, co
  * Pages written here must belong to one sequence of the call alone, and the
  * rows must not overlap the cache.
  * Errors: E_DTYPE, E_SHAPE (limits above; B < 0, T < 1, table_width < 1 or too
- * many tokens, path without T > 1, B * touched pages beyond INT_MAX,
+ * many tokens, path without T > 1, 2 * B * heads * touched pages beyond INT_MAX,
  * out_lengths == lengths), E_NULL (also path without count), E_DEVICE.  B = 0 does nothing.
  */
 int lantern_append_cache(const lantern_cache* cache, const int32_t* table, int table_width, const int32_t* lengths, int B,

@@ -498,7 +498,7 @@ int lantern_append_cache(const lantern_cache* cache, const int32_t* table, int t
     if (B < 0 || T < 1 || table_shape(*cache, table_width) != LANTERN_OK || (path && T < 2)) return LANTERN_E_SHAPE;
     lantern::AppendArgs a;
     a.touched = (int)std::min<int64_t>(table_width, ((int64_t)T + cache->page_tokens - 2) / cache->page_tokens + 1);
-    if ((int64_t)B * a.touched > INT_MAX || (int64_t)B * T > INT_MAX) return LANTERN_E_SHAPE;
+    if (2 * (int64_t)B * a.touched > INT_MAX / cache->heads - 8 || (int64_t)B * T > INT_MAX) return LANTERN_E_SHAPE;
     if (B == 0) return LANTERN_OK;
     a.pairs = 0;
     a.rot = lantern_rotation{};

@@ -1,8 +1,9 @@
 // Appending rows of keys and values to a paged cache (lantern_append_cache), the keys' rotation applied on the way.
 //
-// One workgroup per page that a sequence's rows reach, head, and keys or values.  It brings the rows to LDS in fp32
-// (rotated there: a key is rounded once, to the cache's type), finds their largest magnitude, and writes them: keys as rows
-// [token][D], values turned over, [D][token], which is how the matrix instructions of attend.hip take them.
+// Two kernels.  Few rows (the accepted candidates of a step, single tokens): a wavefront to a page, head and side, keys or values, in
+// registers.  Whole pages (prompts): a workgroup to a page, side and some heads; a key's angles are formed once for all of these.
+// Keys go out as rows [token][D], from registers; values turned over, [D][token], which is how the matrix instructions of attend.hip
+// take them: through LDS.
 //
 // 8-bit pages: value = code * scale.  The scale is the smallest power of two s with largest <= 448 s.  A code has four
 // significant bits under any scale, so nothing is lost against largest / 448 but part of one of e4m3's fifteen binades;
@@ -40,7 +41,7 @@ struct Quantiser {
         return fminf(fmaxf(y, -LARGEST), LARGEST);
     }
     // Four codes; what is not finite becomes NaN, the 8-bit type having no infinity.
-    __device__ __forceinline__ unsigned codes(const float x[4]) const {
+    __device__ __forceinline__ unsigned codes(const float (&x)[4]) const {
         int w = __builtin_amdgcn_cvt_pk_fp8_f32(shrink(x[0]), shrink(x[1]), 0, false);
         w = __builtin_amdgcn_cvt_pk_fp8_f32(shrink(x[2]), shrink(x[3]), w, true);
         unsigned r = (unsigned)w;
@@ -48,10 +49,6 @@ struct Quantiser {
         for (int i = 0; i < 4; ++i)
             if (!finite(x[i])) r = (r & ~(0xFFu << 8 * i)) | NAN_CODE << 8 * i;
         return r;
-    }
-    __device__ __forceinline__ uint8_t code(float x) const {
-        const float four[4] = {x, 0.f, 0.f, 0.f};
-        return (uint8_t)codes(four);
     }
 };
 
@@ -62,160 +59,347 @@ __device__ __forceinline__ uint8_t recode(uint8_t c, float by) {
                   : (uint8_t)NAN_CODE;
 }
 
-// Rows of the page to LDS [rows][D + 1] in fp32; returns the largest finite magnitude this thread has seen.
-template <typename T, bool WIDE>
-__device__ __forceinline__ float bring(const AppendArgs& a, const T* x, int64_t row_stride, int b, int first, int rows, int pairs,
-                                       float* lds) {
-    const int D = a.cache.D, units = rotation_units<4>(pairs, D);
-    float largest = 0.f;
-    for (int i = threadIdx.x; i < rows * units; i += NT) {
-        const int r = i / units, u = i % units, nth = first + r;
-        const int row = a.path && nth > 0 ? a.path[(int64_t)b * (a.T - 1) + nth - 1] + 1 : nth;
-        RotationUnit<T, 4, WIDE> unit;
-        float p[4], q[4];
-        unit.place(u, pairs, D, a.rot.interleaved != 0);
-        unit.load(x + row * row_stride, p, q);
-        if (unit.turned) {
-            unit.angles(a.rot, a.rot.positions + ((int64_t)b * a.T + row) * a.rot.axes, u, false);
-            unit.turn(p, q);
+// What a sequence appends and where.  Every wavefront of a sequence checks all of it and comes to the same end: the sequence is written whole
+// or not at all.
+struct Where {
+    int start, n, page, slot, rows, first;   // rows first .. of the appended n go to the page's slots from `slot` on; rows 0: nothing here
+    int64_t id;
+    __device__ __forceinline__ Where(const AppendArgs& a, int b, int nth_page, bool reports) : start(a.lengths[b]), rows(0) {
+        const int lane = threadIdx.x & (WAVE - 1);
+        if (start < 0) {                       // no sequence here
+            if (reports) a.out_lengths[b] = start;
+            return;
         }
-        RotationUnit<T, 4, false> plain;      // LDS rows of D + 1 floats are not aligned
-        plain.place(u, pairs, D, a.rot.interleaved != 0);
-        plain.store(lds + r * (D + 1), p, q);
+        const int told = a.count ? a.count[b] : a.T - (a.path ? 1 : 0);
+        n = a.path ? told + 1 : told;
+        bool bad = told < 0 || n > a.T || (int64_t)start + n > (int64_t)a.width << a.page_shift;
+        if (!bad && n > 0) {
+            const int first_page = start >> a.page_shift, pages = ((start + n - 1) >> a.page_shift) - first_page + 1;
+            for (int i = lane; i < pages; i += WAVE) {
+                const int p = a.table[(int64_t)b * a.width + first_page + i];
+                bad |= p < 0 || p >= a.cache.pages;
+            }
+            if (a.path)
+                for (int i = lane; i < told; i += WAVE) {
+                    const int node = a.path[(int64_t)b * (a.T - 1) + i];
+                    bad |= node < 0 || node >= a.T - 1;
+                }
+        }
+        bad = __any(bad);
+        if (reports) a.out_lengths[b] = bad ? -2 : start + n;
+        const int w = (start >> a.page_shift) + nth_page;
+        if (bad || (int64_t)w << a.page_shift >= (int64_t)start + n) return;
+        const int lo = max(start, w << a.page_shift), hi = (int)min((int64_t)start + n, (int64_t)(w + 1) << a.page_shift);
+        rows = max(0, hi - lo);
+        slot = lo - (w << a.page_shift);
+        first = lo - start;
+        id = rows > 0 ? a.table[(int64_t)b * a.width + w] : 0;
+    }
+    __device__ __forceinline__ int row_of(const AppendArgs& a, int b, int r) const {
+        const int nth = first + r;
+        return a.path && nth > 0 ? a.path[(int64_t)b * (a.T - 1) + nth - 1] + 1 : nth;
+    }
+};
+
+template <int N>
+__device__ __forceinline__ float largest_of(const float (&p)[N], const float (&q)[N], float largest) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (finite(p[j])) largest = fmaxf(largest, fabsf(p[j]));
-            if (finite(q[j])) largest = fmaxf(largest, fabsf(q[j]));
-        }
+    for (int j = 0; j < N; ++j) {
+        if (finite(p[j])) largest = fmaxf(largest, fabsf(p[j]));
+        if (finite(q[j])) largest = fmaxf(largest, fabsf(q[j]));
     }
     return largest;
 }
 
+// A unit's values into a row of keys.  RUNS: both its runs are four values in a row at multiples of four.
+template <bool EIGHT, typename U>
+__device__ __forceinline__ void write_key(void* row, const U& unit, const Quantiser& to, bool runs, const float (&p)[4], const float (&q)[4]) {
+    if constexpr (EIGHT) {
+        uint8_t* out = static_cast<uint8_t*>(row);
+        if (runs) {
+            const float a[4] = {p[0], unit.inter ? q[0] : p[1], unit.inter ? p[1] : p[2], unit.inter ? q[1] : p[3]};
+            const float b[4] = {unit.inter ? p[2] : q[0], unit.inter ? q[2] : q[1], unit.inter ? p[3] : q[2], q[3]};
+            *reinterpret_cast<unsigned*>(out + unit.o1) = to.codes(a);
+            *reinterpret_cast<unsigned*>(out + unit.o2) = to.codes(b);
+        } else {
+            const unsigned a = to.codes(p), b = to.codes(q);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (j < unit.n1) out[unit.inter ? unit.o1 + 2 * j : unit.o1 + j] = (uint8_t)(a >> 8 * j);
+                if (j < unit.n2) out[unit.inter ? unit.o1 + 2 * j + 1 : unit.o2 + j] = (uint8_t)(b >> 8 * j);
+            }
+        }
+    } else {
+        if (runs) {
+            RotationUnit<float, 4, true> whole;
+            whole.inter = unit.inter;
+            whole.o1 = unit.o1, whole.o2 = unit.o2, whole.n1 = whole.n2 = 4;
+            whole.store(static_cast<bf16*>(row), p, q);
+        } else {
+            RotationUnit<float, 4, false> some;
+            some.inter = unit.inter;
+            some.o1 = unit.o1, some.o2 = unit.o2, some.n1 = unit.n1, some.n2 = unit.n2;
+            some.store(static_cast<bf16*>(row), p, q);
+        }
+    }
+}
+
+// The new scale of a page that holds `slot` tokens already; where it grows, their codes are rounded to it, by the threads of a team.
+__device__ __forceinline__ float rescale(uint8_t* out, float was, float largest, int slot, int D, int page_shift, bool values, int member, int team) {
+    const float need = scale_for(largest), scale = slot ? fmaxf(was, need) : need;
+    if (slot && !(was == scale)) {
+        const float by = was / scale;
+        if (values)
+            for (int i = member; i < D * slot; i += team) {
+                uint8_t* c = out + ((int64_t)(i / slot) << page_shift) + i % slot;
+                *c = recode(*c, by);
+            }
+        else
+            for (int i = member; i < D * slot; i += team) out[i] = recode(out[i], by);
+    }
+    return scale;
+}
+
+// ---- few rows
+
 template <typename T, bool EIGHT>
-__global__ __launch_bounds__(NT) void append_cache_kernel(AppendArgs a) {
-    extern __shared__ float lds[];
-    __shared__ float wave_largest[NW];
-    const int b = blockIdx.x / a.touched, nth_page = blockIdx.x % a.touched, h = blockIdx.y;
-    const bool values = blockIdx.z != 0;
-    const bool reports = nth_page == 0 && h == 0 && !values && threadIdx.x == 0;
-    const int start = a.lengths[b];
-    if (start < 0) {                       // no sequence here
-        if (reports) a.out_lengths[b] = start;
-        return;
-    }
-    // Every workgroup of a sequence checks all of it and comes to the same end: it is written whole or not at all.
-    const int told = a.count ? a.count[b] : a.T - (a.path ? 1 : 0);
-    const int n = a.path ? told + 1 : told;
-    bool bad = told < 0 || n > a.T || (int64_t)start + n > (int64_t)a.width << a.page_shift;
-    if (!bad && n > 0) {
-        const int first_page = start >> a.page_shift, pages = ((start + n - 1) >> a.page_shift) - first_page + 1;
-        for (int i = threadIdx.x; i < pages; i += NT) {
-            const int id = a.table[(int64_t)b * a.width + first_page + i];
-            bad |= id < 0 || id >= a.cache.pages;
+__global__ __launch_bounds__(NT) void append_rows_kernel(AppendArgs a) {
+    const int lane = threadIdx.x & (WAVE - 1), heads = a.cache.heads, D = a.cache.D;
+    const int item = blockIdx.x * NW + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), place = item / heads, h = item % heads;
+    if (place >= 2 * a.B * a.touched) return;
+    const bool values = place & 1;
+    const int b = (place >> 1) / a.touched, nth_page = (place >> 1) % a.touched;
+    const Where w(a, b, nth_page, nth_page == 0 && h == 0 && !values && lane == 0);
+    if (w.rows == 0) return;
+    const Strided s = values ? a.sv : a.sk;
+    const T* const x = static_cast<const T*>(values ? a.v : a.k) + b * s.seq + h * s.head;
+    const int pairs = values ? 0 : a.pairs, units = rotation_units<4>(pairs, D);
+    const bool wide = values ? a.wide_v : a.wide_k;
+    typedef RotationUnit<T, 4, false> Unit;
+    auto bring = [&](int i, Unit& unit, int* r, float (&p)[4], float (&q)[4]) {
+        *r = i / units;
+        const int u = i % units, row = w.row_of(a, b, *r);
+        unit.place(u, pairs, D, a.rot.interleaved != 0);
+        if (wide) {
+            RotationUnit<T, 4, true> whole;
+            whole.inter = unit.inter;
+            whole.o1 = unit.o1, whole.o2 = unit.o2, whole.n1 = whole.n2 = 4;
+            whole.load(x + row * s.row, p, q);
+        } else {
+            unit.load(x + row * s.row, p, q);
         }
-        if (a.path)
-            for (int i = threadIdx.x; i < told; i += NT) {
-                const int node = a.path[(int64_t)b * (a.T - 1) + i];
-                bad |= node < 0 || node >= a.T - 1;
-            }
-    }
-    bad = __syncthreads_or(bad);
-    if (reports) a.out_lengths[b] = bad ? -2 : start + n;
-    if (bad) return;
-    const int w = (start >> a.page_shift) + nth_page;
-    if ((int64_t)w << a.page_shift >= (int64_t)start + n) return;
-    const int lo = max(start, w << a.page_shift), hi = (int)min((int64_t)start + n, (int64_t)(w + 1) << a.page_shift);
-    if (lo >= hi) return;
-    const int rows = hi - lo, slot = lo - (w << a.page_shift);     // slot: where they begin in the page, and how many tokens are before them
-    const int D = a.cache.D, heads = a.cache.heads;
-    const int64_t id = a.table[(int64_t)b * a.width + w], block = id * heads + h;
-
-    float largest;
-    if (values) {
-        const T* x = static_cast<const T*>(a.v) + b * a.sv.seq + h * a.sv.head;
-        largest = a.wide_v ? bring<T, true>(a, x, a.sv.row, b, lo - start, rows, 0, lds) : bring<T, false>(a, x, a.sv.row, b, lo - start, rows, 0, lds);
-    } else {
-        const T* x = static_cast<const T*>(a.k) + b * a.sk.seq + h * a.sk.head;
-        largest = a.wide_k ? bring<T, true>(a, x, a.sk.row, b, lo - start, rows, a.pairs, lds)
-                           : bring<T, false>(a, x, a.sk.row, b, lo - start, rows, a.pairs, lds);
-    }
+        if (unit.turned) {
+            unit.angles(a.rot, a.rot.positions + ((int64_t)b * a.T + row) * a.rot.axes, u, false);
+            unit.turn(p, q);
+        }
+    };
+    const int all = w.rows * units, block_bytes = D << a.page_shift;
+    const int64_t block = w.id * heads + h;
+    Unit unit;
+    int r = 0;
+    float p[4], q[4], scale = 1.f;
+    if (lane < all) bring(lane, unit, &r, p, q);
+    uint8_t* const bytes = static_cast<uint8_t*>(values ? a.cache.v : a.cache.k) + block * block_bytes * (EIGHT ? 1 : 2);
     if constexpr (EIGHT) {
+        float* const scales = values ? a.cache.v_scale : a.cache.k_scale;
+        float largest = lane < all ? largest_of(p, q, 0.f) : 0.f;
+        for (int i = lane + WAVE; i < all; i += WAVE) {      // more than a wavefront holds: turned again for writing
+            Unit other;
+            int of;
+            float c[4], d[4];
+            bring(i, other, &of, c, d);
+            largest = largest_of(c, d, largest);
+        }
         largest = wave_max(largest);
-        if ((threadIdx.x & (WAVE - 1)) == 0) wave_largest[threadIdx.x / WAVE] = largest;
+        const float was = w.slot ? scales[block] : 0.f;
+        scale = rescale(bytes, was, largest, w.slot, D, a.page_shift, values, lane, WAVE);
+        if (lane == 0) scales[block] = scale;
     }
-    __syncthreads();
-
-    if constexpr (EIGHT) {
-        uint8_t* out = static_cast<uint8_t*>(values ? a.cache.v : a.cache.k) + (block << a.page_shift) * D;
-        float* scales = values ? a.cache.v_scale : a.cache.k_scale;
-        const float need = scale_for(fmaxf(fmaxf(wave_largest[0], wave_largest[1]), fmaxf(wave_largest[2], wave_largest[3])));
-        const float was = scales[block], scale = slot ? fmaxf(was, need) : need;
-        const Quantiser to(scale);
-        if (slot && !(was == scale)) {
-            const float by = was / scale;
-            if (values)
-                for (int i = threadIdx.x; i < D * slot; i += NT) {
-                    uint8_t* c = out + ((int64_t)(i / slot) << a.page_shift) + i % slot;
-                    *c = recode(*c, by);
-                }
-            else
-                for (int i = threadIdx.x; i < D * slot; i += NT) out[i] = recode(out[i], by);
+    const Quantiser to(scale);
+    for (int i = lane; i < all; i += WAVE) {
+        if (i > lane) bring(i, unit, &r, p, q);
+        const int slot = w.slot + r;
+        if (!values) {
+            write_key<EIGHT>(bytes + (int64_t)slot * D * (EIGHT ? 1 : 2), unit, to, wide && unit.n1 == 4 && unit.n2 == 4, p, q);
+            continue;
         }
-        if (values) {
-            // four tokens of a column at a time; a group that is not all new is written byte by byte
-            const int g0 = slot / 4, groups = (slot + rows + 3) / 4 - g0;
-            for (int i = threadIdx.x; i < D * groups; i += NT) {
-                const int d = i / groups, at = (g0 + i % groups) * 4;
-                uint8_t* c = out + ((int64_t)d << a.page_shift) + at;
-                float x[4];
+        const unsigned cp = EIGHT ? to.codes(p) : 0u, cq = EIGHT ? to.codes(q) : 0u;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int r = at + j - slot;
-                    x[j] = r >= 0 && r < rows ? lds[r * (D + 1) + d] : 0.f;
-                }
-                const unsigned four = to.codes(x);
-                if (at >= slot && at + 4 <= slot + rows)
-                    *reinterpret_cast<unsigned*>(c) = four;
-                else
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (at + j >= slot && at + j < slot + rows) c[j] = (uint8_t)(four >> 8 * j);
-            }
-        } else {
-            for (int i = threadIdx.x; i < rows * (D / 4); i += NT) {
-                const int r = i / (D / 4), d = i % (D / 4) * 4;
-                const float x[4] = {lds[r * (D + 1) + d], lds[r * (D + 1) + d + 1], lds[r * (D + 1) + d + 2], lds[r * (D + 1) + d + 3]};
-                *reinterpret_cast<unsigned*>(out + (slot + r) * D + d) = to.codes(x);
-            }
-        }
-        __syncthreads();      // every thread has read the old scale
-        if (threadIdx.x == 0) scales[block] = scale;
-    } else {
-        bf16* out = static_cast<bf16*>(values ? a.cache.v : a.cache.k) + (block << a.page_shift) * D;
-        if (values) {
-            for (int i = threadIdx.x; i < D * rows; i += NT) {
-                const int d = i / rows, r = i % rows;
-                out[((int64_t)d << a.page_shift) + slot + r] = (bf16)lds[r * (D + 1) + d];
-            }
-        } else {
-            for (int i = threadIdx.x; i < rows * (D / 2); i += NT) {
-                const int r = i / (D / 2), d = i % (D / 2) * 2;
-                const bf16x2 two = {(bf16)lds[r * (D + 1) + d], (bf16)lds[r * (D + 1) + d + 1]};
-                *reinterpret_cast<bf16x2*>(out + (slot + r) * D + d) = two;
+        for (int j = 0; j < 4; ++j) {      // D is a multiple of 8: units of values are whole
+            const int64_t at = ((int64_t)(unit.o1 + j) << a.page_shift) + slot, next = at + ((int64_t)4 << a.page_shift);
+            if constexpr (EIGHT) {
+                bytes[at] = (uint8_t)(cp >> 8 * j);
+                bytes[next] = (uint8_t)(cq >> 8 * j);
+            } else {
+                reinterpret_cast<bf16*>(bytes)[at] = (bf16)p[j];
+                reinterpret_cast<bf16*>(bytes)[next] = (bf16)q[j];
             }
         }
     }
 }
 
-static size_t lds_bytes(const lantern_cache& c) { return sizeof(float) * c.page_tokens * (c.D + 1); }
+// ---- whole pages.  EACH: most units of a page's keys to a thread.
+
+__device__ __forceinline__ float block_max(float x, float* waves) {
+    x = wave_max(x);
+    __syncthreads();      // what was there has been read
+    if ((threadIdx.x & (WAVE - 1)) == 0) waves[threadIdx.x / WAVE] = x;
+    __syncthreads();
+    return fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3]));
+}
+
+template <typename T, bool EIGHT, int EACH, bool WIDE>
+__device__ __forceinline__ void append_keys(const AppendArgs& a, const Where& w, int b, int h, int last, float* waves) {
+    const int D = a.cache.D, units = rotation_units<4>(a.pairs, D), all = w.rows * units;
+    RotationUnit<T, 4, WIDE> unit[EACH];
+    int64_t from[EACH];
+    int at[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        const int i = min((int)threadIdx.x + e * NT, all - 1), r = i / units, u = i % units, row = w.row_of(a, b, r);
+        unit[e].place(u, a.pairs, D, a.rot.interleaved != 0);
+        if (unit[e].turned) unit[e].angles(a.rot, a.rot.positions + ((int64_t)b * a.T + row) * a.rot.axes, u, false);
+        from[e] = row * a.sk.row;
+        at[e] = (w.slot + r) * D;
+    }
+    for (; h < last; ++h) {
+        const T* const x = static_cast<const T*>(a.k) + b * a.sk.seq + h * a.sk.head;
+        const int64_t block = w.id * a.cache.heads + h;
+        float p[EACH][4], q[EACH][4], largest = 0.f, scale = 1.f;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) unit[e].load(x + from[e], p[e], q[e]);
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            unit[e].turn(p[e], q[e]);
+            largest = largest_of(p[e], q[e], largest);
+        }
+        uint8_t* const bytes = static_cast<uint8_t*>(a.cache.k) + (block << a.page_shift) * D * (EIGHT ? 1 : 2);
+        if constexpr (EIGHT) {
+            const float was = w.slot ? a.cache.k_scale[block] : 0.f;
+            largest = block_max(largest, waves);      // and every thread has read the scale
+            scale = rescale(bytes, was, largest, w.slot, D, a.page_shift, false, threadIdx.x, NT);
+            if (threadIdx.x == 0) a.cache.k_scale[block] = scale;
+        }
+        const Quantiser to(scale);
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+            if ((int)threadIdx.x + e * NT < all) write_key<EIGHT>(bytes + (int64_t)at[e] * (EIGHT ? 1 : 2), unit[e], to, WIDE, p[e], q[e]);
+    }
+}
+
+template <typename T, bool EIGHT>
+__device__ __forceinline__ void append_values(const AppendArgs& a, const Where& w, int b, int h, int last, float* waves, T* lds) {
+    const int D = a.cache.D, per_row = D / 8, all = w.rows * per_row, stride = D + 4;
+    for (; h < last; ++h) {
+        const T* const x = static_cast<const T*>(a.v) + b * a.sv.seq + h * a.sv.head;
+        const int64_t block = w.id * a.cache.heads + h;
+        uint8_t* const bytes = static_cast<uint8_t*>(a.cache.v) + (block << a.page_shift) * D * (EIGHT ? 1 : 2);
+        const float was = EIGHT && w.slot ? a.cache.v_scale[block] : 0.f;
+        float largest = 0.f, scale = 1.f;
+        __syncthreads();      // the head before has been written
+        for (int i = threadIdx.x; i < all; i += NT) {
+            const int r = i / per_row, d = i % per_row * 8;
+            const T* const from = x + w.row_of(a, b, r) * a.sv.row + d;
+            typedef typename Vec<T, 4>::type Four;
+            Four p, q;
+            if (a.wide_v) {
+                p = *reinterpret_cast<const Four*>(from);
+                q = *reinterpret_cast<const Four*>(from + 4);
+            } else {
+                p = Four{from[0], from[1], from[2], from[3]};
+                q = Four{from[4], from[5], from[6], from[7]};
+            }
+            *reinterpret_cast<Four*>(lds + r * stride + d) = p;
+            *reinterpret_cast<Four*>(lds + r * stride + d + 4) = q;
+            if constexpr (EIGHT) {
+                const float c[4] = {(float)p[0], (float)p[1], (float)p[2], (float)p[3]}, e[4] = {(float)q[0], (float)q[1], (float)q[2], (float)q[3]};
+                largest = largest_of(c, e, largest);
+            }
+        }
+        if constexpr (EIGHT) {
+            largest = block_max(largest, waves);      // and the rows are there
+            scale = rescale(bytes, was, largest, w.slot, D, a.page_shift, true, threadIdx.x, NT);
+            if (threadIdx.x == 0) a.cache.v_scale[block] = scale;
+        } else {
+            __syncthreads();
+        }
+        const Quantiser to(scale);
+        // 16 bytes of an element at a time; a piece that is not all new is written token by token
+        constexpr int AT_ONCE = EIGHT ? 16 : 8;
+        const int g0 = w.slot / AT_ONCE, groups = (w.slot + w.rows + AT_ONCE - 1) / AT_ONCE - g0;
+        for (int i = threadIdx.x; i < D * groups; i += NT) {
+            const int d = i / groups, at = (g0 + i % groups) * AT_ONCE;
+            u32x4 out;
+            const bool whole = at >= w.slot && at + AT_ONCE <= w.slot + w.rows;
+            float v[AT_ONCE];
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j) v[j] = (float)lds[min(max(at + j - w.slot, 0), w.rows - 1) * stride + d];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if constexpr (EIGHT) {
+                    const float four[4] = {v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]};
+                    out[k] = to.codes(four);
+                } else {
+                    out[k] = __builtin_bit_cast(unsigned, bf16x2{(bf16)v[2 * k], (bf16)v[2 * k + 1]});
+                }
+            }
+            const int64_t place = ((int64_t)d << a.page_shift) + at;
+            if (whole) {
+                *reinterpret_cast<u32x4*>(bytes + place * (EIGHT ? 1 : 2)) = out;
+            } else {
+#pragma unroll
+                for (int j = 0; j < AT_ONCE; ++j) {
+                    if (at + j < w.slot || at + j >= w.slot + w.rows) continue;
+                    if constexpr (EIGHT) bytes[place + j] = (uint8_t)(out[j / 4] >> 8 * (j % 4));
+                    else reinterpret_cast<uint16_t*>(bytes)[place + j] = (uint16_t)(out[j / 2] >> 16 * (j % 2));
+                }
+            }
+        }
+    }
+}
+
+template <typename T, bool EIGHT, int EACH>
+__global__ __launch_bounds__(NT) void append_pages_kernel(AppendArgs a, int heads_each) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float waves[NW];
+    const int b = blockIdx.x / a.touched, nth_page = blockIdx.x % a.touched, h = blockIdx.y * heads_each, last = min(a.cache.heads, h + heads_each);
+    const bool values = blockIdx.z != 0;
+    const Where w(a, b, nth_page, nth_page == 0 && h == 0 && !values && threadIdx.x == 0);
+    if (w.rows == 0) return;
+    if (values) append_values<T, EIGHT>(a, w, b, h, last, waves, reinterpret_cast<T*>(lds));
+    else if (a.wide_k) append_keys<T, EIGHT, EACH, true>(a, w, b, h, last, waves);
+    else append_keys<T, EIGHT, EACH, false>(a, w, b, h, last, waves);
+}
+
+template <typename T>
+static size_t lds_bytes(const lantern_cache& c) { return sizeof(T) * c.page_tokens * (c.D + 4); }
+
+template <typename T, bool EIGHT, int EACH>
+static hipError_t launch_pages(const AppendArgs& a, hipStream_t stream) {
+    const size_t lds = lds_bytes<T>(a.cache);
+    const hipError_t e = allow_lds<append_pages_kernel<T, EIGHT, EACH>>(lds);
+    if (e != hipSuccess) return e;
+    // Several heads to a workgroup, for whose keys the angles are formed once, while there are four workgroups and more to a CU.
+    const int64_t places = 2 * (int64_t)a.B * a.touched;
+    const int each = (int)std::max<int64_t>(1, std::min<int64_t>(a.cache.heads, places * a.cache.heads / 1024));
+    hipLaunchKernelGGL((append_pages_kernel<T, EIGHT, EACH>), dim3(a.B * a.touched, (a.cache.heads + each - 1) / each, 2), dim3(NT), lds, stream, a,
+                       each);
+    return hipGetLastError();
+}
 
 template <typename T, bool EIGHT>
 static hipError_t launch(const AppendArgs& a, hipStream_t stream) {
-    const size_t lds = lds_bytes(a.cache);
-    const hipError_t e = allow_lds<append_cache_kernel<T, EIGHT>>(lds);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((append_cache_kernel<T, EIGHT>), dim3(a.B * a.touched, a.cache.heads, 2), dim3(NT), lds, stream, a);
-    return hipGetLastError();
+    const int units = std::max(rotation_units<4>(a.pairs, a.cache.D), a.cache.D / 8);
+    // A wavefront holds 64 units: up to four times that in rows, and the accepted candidates of a tree, which are few
+    if (a.path || a.T * units <= 4 * WAVE) {
+        const int64_t items = 2 * (int64_t)a.B * a.touched * a.cache.heads;
+        hipLaunchKernelGGL((append_rows_kernel<T, EIGHT>), dim3((unsigned)((items + NW - 1) / NW)), dim3(NT), 0, stream, a);
+        return hipGetLastError();
+    }
+    const int each = (a.cache.page_tokens * units + NT - 1) / NT;      // 9 at most: pages of 128, 17 units of a head
+    if (each <= 2) return launch_pages<T, EIGHT, 2>(a, stream);
+    if (each <= 4) return launch_pages<T, EIGHT, 4>(a, stream);
+    return launch_pages<T, EIGHT, 9>(a, stream);
 }
 
 hipError_t launch_append_cache(const AppendArgs& a, int dtype, hipStream_t stream) {
@@ -226,9 +410,13 @@ hipError_t launch_append_cache(const AppendArgs& a, int dtype, hipStream_t strea
 
 template <typename T, bool EIGHT>
 static hipError_t prepare(const lantern_cache& c) {
-    hipFuncAttributes attr;
-    const hipError_t e = hipFuncGetAttributes(&attr, reinterpret_cast<const void*>(&append_cache_kernel<T, EIGHT>));
-    return e != hipSuccess ? e : allow_lds<append_cache_kernel<T, EIGHT>>(lds_bytes(c));
+    hipFuncAttributes attr;   // the runtime loads all of a file's kernels together
+    hipError_t e = hipFuncGetAttributes(&attr, reinterpret_cast<const void*>(&append_rows_kernel<T, EIGHT>));
+    const size_t lds = lds_bytes<T>(c);
+    if (e == hipSuccess) e = allow_lds<append_pages_kernel<T, EIGHT, 2>>(lds);
+    if (e == hipSuccess) e = allow_lds<append_pages_kernel<T, EIGHT, 4>>(lds);
+    if (e == hipSuccess) e = allow_lds<append_pages_kernel<T, EIGHT, 9>>(lds);
+    return e;
 }
 
 hipError_t prepare_append(int dtype, const lantern_cache& c) {

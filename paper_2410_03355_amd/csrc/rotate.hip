@@ -13,6 +13,8 @@
 
 namespace lantern {
 
+constexpr int AT_ONCE = 4;      // heads loaded together: an output may be its input, so no load passes a store
+
 template <typename T, int NP, bool WIDE>
 __global__ __launch_bounds__(NT) void rotate_axes_kernel(RotateArgs a) {
     const int units = rotation_units<NP>(a.pairs, a.D);
@@ -25,16 +27,24 @@ __global__ __launch_bounds__(NT) void rotate_axes_kernel(RotateArgs a) {
     if (unit.turned) unit.angles(a.rot, a.rot.positions + token * a.rot.axes, u, a.inverse != 0);
     const int heads = a.q_heads + a.k_heads;
     const int first = blockIdx.y * a.heads_per_block, last = min(heads, first + a.heads_per_block);
-#pragma unroll 4
-    for (int h = first; h < last; ++h) {
-        const bool of_q = h < a.q_heads;
-        const int hh = of_q ? h : h - a.q_heads;
-        const T* x = static_cast<const T*>(of_q ? a.q : a.k) + (of_q ? token * a.sq.row + hh * a.sq.head : token * a.sk.row + hh * a.sk.head);
-        T* y = static_cast<T*>(of_q ? a.out_q : a.out_k) + (of_q ? token * a.soq.row + hh * a.soq.head : token * a.sok.row + hh * a.sok.head);
-        float p[NP], q[NP];
-        unit.load(x, p, q);
-        unit.turn(p, q);
-        unit.store(y, p, q);
+    auto in = [&](int h) {
+        return h < a.q_heads ? static_cast<const T*>(a.q) + token * a.sq.row + h * a.sq.head
+                             : static_cast<const T*>(a.k) + token * a.sk.row + (h - a.q_heads) * a.sk.head;
+    };
+    auto out = [&](int h) {
+        return h < a.q_heads ? static_cast<T*>(a.out_q) + token * a.soq.row + h * a.soq.head
+                             : static_cast<T*>(a.out_k) + token * a.sok.row + (h - a.q_heads) * a.sok.head;
+    };
+    for (int h = first; h < last; h += AT_ONCE) {      // the last heads again where fewer are left: loaded, not written
+        float p[AT_ONCE][NP], q[AT_ONCE][NP];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) unit.load(in(min(h + i, last - 1)), p[i], q[i]);
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            if (h + i >= last) break;
+            unit.turn(p[i], q[i]);
+            unit.store(out(h + i), p[i], q[i]);
+        }
     }
 }
 

@@ -4,8 +4,7 @@
 //   y1 = x1 cos phi - x2 sin phi,  y2 = x1 sin phi + x2 cos phi
 // The pair is (x[2j], x[2j+1]) (interleaved) or (x[j], x[j+P]), P pairs in all; elements from 2P on stay as they are.
 // The angle is formed in fp64 and so are cosine and sine, which are then rounded once: a position of 10^5 in fp32 would
-// leave an error of 2^-24 * 10^5 in the angle.  They cost some 100 fp64 instructions for a pair of a token and serve all
-// of its heads.
+// leave an error of 2^-24 * 10^5 in the angle.  They serve all heads of a token.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -29,13 +28,31 @@ struct Vec {
     typedef T type __attribute__((ext_vector_type(N)));
 };
 
-// cos and sin of position * freq.
+// cos and sin of position * freq: the product in fp64, less k quarter turns (pi / 2 in two parts, the fused steps exact but for
+// their last), then the Taylor sums to y^13 and y^12 with |y| <= pi / 4: their errors, y^15 / 15! and y^14 / 14!, are under 2^-40, and the
+// results rounded to fp32 once.  Some 25 fp64 operations.
 __device__ __forceinline__ void angle(int32_t position, float freq, float* c, float* s) {
-    constexpr double PER_PI = 0.318309886183790671537767526745;
-    double sd, cd;
-    sincospi((double)position * (double)freq * PER_PI, &sd, &cd);
-    *c = (float)cd;
-    *s = (float)sd;
+    constexpr double QUARTERS = 0.63661977236758134308, HALF_PI = 1.5707963267948966192, HALF_PI_LOW = 6.1232339957367660359e-17;
+    const double x = (double)position * (double)freq;
+    const double k = rint(x * QUARTERS);
+    const double y = __builtin_fma(-k, HALF_PI_LOW, __builtin_fma(-k, HALF_PI, x)), z = y * y;
+    double sn = 1.0 / 6227020800.0, cs = 1.0 / 479001600.0;
+    sn = __builtin_fma(sn, z, -1.0 / 39916800.0);
+    sn = __builtin_fma(sn, z, 1.0 / 362880.0);
+    sn = __builtin_fma(sn, z, -1.0 / 5040.0);
+    sn = __builtin_fma(sn, z, 1.0 / 120.0);
+    sn = __builtin_fma(sn, z, -1.0 / 6.0);
+    sn = __builtin_fma(sn * z, y, y);
+    cs = __builtin_fma(cs, z, -1.0 / 3628800.0);
+    cs = __builtin_fma(cs, z, 1.0 / 40320.0);
+    cs = __builtin_fma(cs, z, -1.0 / 720.0);
+    cs = __builtin_fma(cs, z, 1.0 / 24.0);
+    cs = __builtin_fma(cs, z, -0.5);
+    cs = __builtin_fma(cs, z, 1.0);
+    const int turn = (int)(k - 4.0 * floor(k * 0.25));      // 0 .. 3
+    const float a = (float)(turn & 1 ? sn : cs), b = (float)(turn & 1 ? cs : sn);
+    *c = turn == 1 || turn == 2 ? -a : a;
+    *s = turn & 2 ? -b : b;
 }
 
 __device__ __forceinline__ int axis_of(const lantern_rotation& r, int j) {
