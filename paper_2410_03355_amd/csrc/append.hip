@@ -35,19 +35,21 @@ __device__ __forceinline__ float scale_for(float largest) {
 
 struct Quantiser {
     float scale, per;      // per: 1 / scale, exact, or 0 where the scale is no power of two (a cache filled by others)
-    __device__ __forceinline__ explicit Quantiser(float s) : scale(s), per((__float_as_uint(s) & 0x7FFFFFu) ? 0.f : 1.f / s) {}
-    __device__ __forceinline__ float shrink(float x) const {
-        const float y = per != 0.f ? x * per : x / scale;
-        return fminf(fmaxf(y, -LARGEST), LARGEST);
-    }
-    // Four codes; what is not finite becomes NaN, the 8-bit type having no infinity.
+    bool odd;              // not all values are finite
+    __device__ __forceinline__ Quantiser(float s, bool o) : scale(s), per((__float_as_uint(s) & 0x7FFFFFu) ? 0.f : 1.f / s), odd(o) {}
+    // Four codes.  Finite values are within 448 scales, so they need no limit; what is not finite becomes NaN, the 8-bit type having no
+    // infinity.
     __device__ __forceinline__ unsigned codes(const float (&x)[4]) const {
-        int w = __builtin_amdgcn_cvt_pk_fp8_f32(shrink(x[0]), shrink(x[1]), 0, false);
-        w = __builtin_amdgcn_cvt_pk_fp8_f32(shrink(x[2]), shrink(x[3]), w, true);
-        unsigned r = (unsigned)w;
+        float y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (!finite(x[i])) r = (r & ~(0xFFu << 8 * i)) | NAN_CODE << 8 * i;
+        for (int i = 0; i < 4; ++i) y[i] = per != 0.f ? x[i] * per : x[i] / scale;
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+        unsigned r = (unsigned)w;
+        if (odd)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (!finite(x[i])) r = (r & ~(0xFFu << 8 * i)) | NAN_CODE << 8 * i;
         return r;
     }
 };
@@ -101,15 +103,23 @@ struct Where {
     }
 };
 
-template <int N>
-__device__ __forceinline__ float largest_of(const float (&p)[N], const float (&q)[N], float largest) {
+// The largest magnitude as bits, which order like it; from ODD on a value is not finite.
+constexpr int ODD = 0x7F800000;
+__device__ __forceinline__ int largest_of(const float (&p)[4], const float (&q)[4], int largest) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-        if (finite(p[j])) largest = fmaxf(largest, fabsf(p[j]));
-        if (finite(q[j])) largest = fmaxf(largest, fabsf(q[j]));
+    for (int j = 0; j < 4; ++j) largest = max(largest, max(__float_as_int(p[j]) & 0x7FFFFFFF, __float_as_int(q[j]) & 0x7FFFFFFF));
+    return largest;
+}
+// The same of the finite ones.
+__device__ __forceinline__ int largest_finite(const float (&p)[4], const float (&q)[4], int largest) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int a = __float_as_int(p[j]) & 0x7FFFFFFF, b = __float_as_int(q[j]) & 0x7FFFFFFF;
+        largest = max(largest, max(a < ODD ? a : 0, b < ODD ? b : 0));
     }
     return largest;
 }
+__device__ __forceinline__ int wave_max_i(int x) { return __builtin_amdgcn_readlane(wave_scan_i<OpMax>(x, 0), WAVE - 1); }
 
 // A unit's values into a row of keys.  RUNS: both its runs are four values in a row at multiples of four.
 template <bool EIGHT, typename U>
@@ -145,8 +155,8 @@ __device__ __forceinline__ void write_key(void* row, const U& unit, const Quanti
 }
 
 // The new scale of a page that holds `slot` tokens already; where it grows, their codes are rounded to it, by the threads of a team.
-__device__ __forceinline__ float rescale(uint8_t* out, float was, float largest, int slot, int D, int page_shift, bool values, int member, int team) {
-    const float need = scale_for(largest), scale = slot ? fmaxf(was, need) : need;
+__device__ __forceinline__ float rescale(uint8_t* out, float was, int largest, int slot, int D, int page_shift, bool values, int member, int team) {
+    const float need = scale_for(__int_as_float(largest)), scale = slot ? fmaxf(was, need) : need;
     if (slot && !(was == scale)) {
         const float by = was / scale;
         if (values)
@@ -198,11 +208,12 @@ __global__ __launch_bounds__(NT) void append_rows_kernel(AppendArgs a) {
     Unit unit;
     int r = 0;
     float p[4], q[4], scale = 1.f;
+    bool odd = false;
     if (lane < all) bring(lane, unit, &r, p, q);
     uint8_t* const bytes = static_cast<uint8_t*>(values ? a.cache.v : a.cache.k) + block * block_bytes * (EIGHT ? 1 : 2);
     if constexpr (EIGHT) {
         float* const scales = values ? a.cache.v_scale : a.cache.k_scale;
-        float largest = lane < all ? largest_of(p, q, 0.f) : 0.f;
+        int largest = lane < all ? largest_of(p, q, 0) : 0;
         for (int i = lane + WAVE; i < all; i += WAVE) {      // more than a wavefront holds: turned again for writing
             Unit other;
             int of;
@@ -210,12 +221,24 @@ __global__ __launch_bounds__(NT) void append_rows_kernel(AppendArgs a) {
             bring(i, other, &of, c, d);
             largest = largest_of(c, d, largest);
         }
-        largest = wave_max(largest);
+        largest = wave_max_i(largest);
+        odd = largest >= ODD;
+        if (odd) {
+            largest = 0;
+            for (int i = lane; i < all; i += WAVE) {
+                Unit other;
+                int of;
+                float c[4], d[4];
+                bring(i, other, &of, c, d);
+                largest = largest_finite(c, d, largest);
+            }
+            largest = wave_max_i(largest);
+        }
         const float was = w.slot ? scales[block] : 0.f;
         scale = rescale(bytes, was, largest, w.slot, D, a.page_shift, values, lane, WAVE);
         if (lane == 0) scales[block] = scale;
     }
-    const Quantiser to(scale);
+    const Quantiser to(scale, odd);
     for (int i = lane; i < all; i += WAVE) {
         if (i > lane) bring(i, unit, &r, p, q);
         const int slot = w.slot + r;
@@ -238,92 +261,146 @@ __global__ __launch_bounds__(NT) void append_rows_kernel(AppendArgs a) {
     }
 }
 
-// ---- whole pages.  EACH: most units of a page's keys to a thread.
+// ---- whole pages, of rows one after the other (no path).  The rows of the next head are asked for before this one's are worked on.
 
-__device__ __forceinline__ float block_max(float x, float* waves) {
-    x = wave_max(x);
+__device__ __forceinline__ int block_max(int x, int* waves) {
+    x = wave_max_i(x);
     __syncthreads();      // what was there has been read
     if ((threadIdx.x & (WAVE - 1)) == 0) waves[threadIdx.x / WAVE] = x;
     __syncthreads();
-    return fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3]));
+    return max(max(waves[0], waves[1]), max(waves[2], waves[3]));
 }
 
+// A thread has one unit of EACH rows at most, NT / units apart.
 template <typename T, bool EIGHT, int EACH, bool WIDE>
-__device__ __forceinline__ void append_keys(const AppendArgs& a, const Where& w, int b, int h, int last, float* waves) {
-    const int D = a.cache.D, units = rotation_units<4>(a.pairs, D), all = w.rows * units;
-    RotationUnit<T, 4, WIDE> unit[EACH];
-    int64_t from[EACH];
-    int at[EACH];
-#pragma unroll
-    for (int e = 0; e < EACH; ++e) {
-        const int i = min((int)threadIdx.x + e * NT, all - 1), r = i / units, u = i % units, row = w.row_of(a, b, r);
-        unit[e].place(u, a.pairs, D, a.rot.interleaved != 0);
-        if (unit[e].turned) unit[e].angles(a.rot, a.rot.positions + ((int64_t)b * a.T + row) * a.rot.axes, u, false);
-        from[e] = row * a.sk.row;
-        at[e] = (w.slot + r) * D;
-    }
-    for (; h < last; ++h) {
-        const T* const x = static_cast<const T*>(a.k) + b * a.sk.seq + h * a.sk.head;
-        const int64_t block = w.id * a.cache.heads + h;
-        float p[EACH][4], q[EACH][4], largest = 0.f, scale = 1.f;
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) unit[e].load(x + from[e], p[e], q[e]);
+__device__ __forceinline__ void append_keys(const AppendArgs& a, const Where& w, int b, int h, int last, int* waves) {
+    const int D = a.cache.D, units = rotation_units<4>(a.pairs, D), at_once = NT / units;
+    const int u = threadIdx.x % units, mine = threadIdx.x / units;      // threads from at_once * units on have nothing
+    RotationUnit<T, 4, WIDE> unit;
+    unit.place(u, a.pairs, D, a.rot.interleaved != 0);
+    float c[EACH][4], s[EACH][4];
+    if (unit.turned) {
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
-            unit[e].turn(p[e], q[e]);
-            largest = largest_of(p[e], q[e], largest);
+            const int row = w.first + min(mine + e * at_once, w.rows - 1);
+            unit.angles(a.rot, a.rot.positions + ((int64_t)b * a.T + row) * a.rot.axes, u, false);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) c[e][j] = unit.c[j], s[e][j] = unit.s[j];
         }
+    }
+    T p[EACH][4], q[EACH][4];
+    auto ask = [&](int head) {
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int64_t row = w.first + min(mine + e * at_once, w.rows - 1);
+            unit.load_as(static_cast<const T*>(a.k) + b * a.sk.seq + head * a.sk.head + row * a.sk.row, p[e], q[e]);
+        }
+    };
+    ask(h);
+    for (; h < last; ++h) {
+        const int64_t block = w.id * a.cache.heads + h;
+        float x[EACH][4], y[EACH][4], scale = 1.f;
+        int largest = 0;
+        bool odd = false;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[e][j] = (float)p[e][j], y[e][j] = (float)q[e][j];
+                unit.c[j] = c[e][j], unit.s[j] = s[e][j];
+            }
+            unit.turn(x[e], y[e]);
+            largest = largest_of(x[e], y[e], largest);
+        }
+        ask(min(h + 1, last - 1));
         uint8_t* const bytes = static_cast<uint8_t*>(a.cache.k) + (block << a.page_shift) * D * (EIGHT ? 1 : 2);
         if constexpr (EIGHT) {
             const float was = w.slot ? a.cache.k_scale[block] : 0.f;
             largest = block_max(largest, waves);      // and every thread has read the scale
+            odd = largest >= ODD;
+            if (odd) {
+                largest = 0;
+#pragma unroll
+                for (int e = 0; e < EACH; ++e) largest = largest_finite(x[e], y[e], largest);
+                largest = block_max(largest, waves);
+            }
             scale = rescale(bytes, was, largest, w.slot, D, a.page_shift, false, threadIdx.x, NT);
             if (threadIdx.x == 0) a.cache.k_scale[block] = scale;
         }
-        const Quantiser to(scale);
+        const Quantiser to(scale, odd);
 #pragma unroll
-        for (int e = 0; e < EACH; ++e)
-            if ((int)threadIdx.x + e * NT < all) write_key<EIGHT>(bytes + (int64_t)at[e] * (EIGHT ? 1 : 2), unit[e], to, WIDE, p[e], q[e]);
+        for (int e = 0; e < EACH; ++e) {
+            const int r = mine + e * at_once;
+            if (mine < at_once && r < w.rows)
+                write_key<EIGHT>(bytes + (int64_t)(w.slot + r) * D * (EIGHT ? 1 : 2), unit, to, WIDE, x[e], y[e]);
+        }
     }
 }
 
 template <typename T, bool EIGHT>
-__device__ __forceinline__ void append_values(const AppendArgs& a, const Where& w, int b, int h, int last, float* waves, T* lds) {
+__device__ __forceinline__ void append_values(const AppendArgs& a, const Where& w, int b, int h, int last, int* waves, T* lds) {
+    typedef typename Vec<T, 4>::type Four;
+    constexpr int MOST = 4;      // pieces of 8 elements that a thread asks for ahead: all of a page's up to 64 tokens of 128
     const int D = a.cache.D, per_row = D / 8, all = w.rows * per_row, stride = D + 4;
+    Four p[MOST], q[MOST];
+    auto load = [&](int head, int i, Four& x, Four& y) {
+        const T* const from = static_cast<const T*>(a.v) + b * a.sv.seq + head * a.sv.head + (int64_t)(w.first + i / per_row) * a.sv.row + i % per_row * 8;
+        if (a.wide_v) {
+            x = *reinterpret_cast<const Four*>(from);
+            y = *reinterpret_cast<const Four*>(from + 4);
+        } else {
+            x = Four{from[0], from[1], from[2], from[3]};
+            y = Four{from[4], from[5], from[6], from[7]};
+        }
+    };
+    auto ask = [&](int head) {
+#pragma unroll
+        for (int e = 0; e < MOST; ++e) load(head, min((int)threadIdx.x + e * NT, all - 1), p[e], q[e]);
+    };
+    ask(h);
     for (; h < last; ++h) {
-        const T* const x = static_cast<const T*>(a.v) + b * a.sv.seq + h * a.sv.head;
         const int64_t block = w.id * a.cache.heads + h;
         uint8_t* const bytes = static_cast<uint8_t*>(a.cache.v) + (block << a.page_shift) * D * (EIGHT ? 1 : 2);
         const float was = EIGHT && w.slot ? a.cache.v_scale[block] : 0.f;
-        float largest = 0.f, scale = 1.f;
+        float scale = 1.f;
+        int largest = 0;
+        bool odd = false;
         __syncthreads();      // the head before has been written
-        for (int i = threadIdx.x; i < all; i += NT) {
-            const int r = i / per_row, d = i % per_row * 8;
-            const T* const from = x + w.row_of(a, b, r) * a.sv.row + d;
-            typedef typename Vec<T, 4>::type Four;
-            Four p, q;
-            if (a.wide_v) {
-                p = *reinterpret_cast<const Four*>(from);
-                q = *reinterpret_cast<const Four*>(from + 4);
-            } else {
-                p = Four{from[0], from[1], from[2], from[3]};
-                q = Four{from[4], from[5], from[6], from[7]};
-            }
-            *reinterpret_cast<Four*>(lds + r * stride + d) = p;
-            *reinterpret_cast<Four*>(lds + r * stride + d + 4) = q;
+        auto put = [&](int i, const Four& x, const Four& y) {
+            T* const to = lds + i / per_row * stride + i % per_row * 8;
+            *reinterpret_cast<Four*>(to) = x;
+            *reinterpret_cast<Four*>(to + 4) = y;
             if constexpr (EIGHT) {
-                const float c[4] = {(float)p[0], (float)p[1], (float)p[2], (float)p[3]}, e[4] = {(float)q[0], (float)q[1], (float)q[2], (float)q[3]};
+                const float c[4] = {(float)x[0], (float)x[1], (float)x[2], (float)x[3]}, e[4] = {(float)y[0], (float)y[1], (float)y[2], (float)y[3]};
                 largest = largest_of(c, e, largest);
             }
+        };
+#pragma unroll
+        for (int e = 0; e < MOST; ++e) put(min((int)threadIdx.x + e * NT, all - 1), p[e], q[e]);
+        for (int i = threadIdx.x + MOST * NT; i < all; i += NT) {
+            Four x, y;
+            load(h, i, x, y);
+            put(i, x, y);
         }
+        ask(min(h + 1, last - 1));
         if constexpr (EIGHT) {
             largest = block_max(largest, waves);      // and the rows are there
+            odd = largest >= ODD;
+            if (odd) {
+                largest = 0;
+                for (int i = threadIdx.x; i < all; i += NT) {
+                    const T* const x = lds + i / per_row * stride + i % per_row * 8;
+                    const float c[4] = {(float)x[0], (float)x[1], (float)x[2], (float)x[3]}, e[4] = {(float)x[4], (float)x[5], (float)x[6], (float)x[7]};
+                    largest = largest_finite(c, e, largest);
+                }
+                largest = block_max(largest, waves);
+            }
             scale = rescale(bytes, was, largest, w.slot, D, a.page_shift, true, threadIdx.x, NT);
             if (threadIdx.x == 0) a.cache.v_scale[block] = scale;
         } else {
             __syncthreads();
         }
-        const Quantiser to(scale);
+        const Quantiser to(scale, odd);
         // 16 bytes of an element at a time; a piece that is not all new is written token by token
         constexpr int AT_ONCE = EIGHT ? 16 : 8;
         const int g0 = w.slot / AT_ONCE, groups = (w.slot + w.rows + AT_ONCE - 1) / AT_ONCE - g0;
@@ -361,7 +438,7 @@ __device__ __forceinline__ void append_values(const AppendArgs& a, const Where& 
 template <typename T, bool EIGHT, int EACH>
 __global__ __launch_bounds__(NT) void append_pages_kernel(AppendArgs a, int heads_each) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    __shared__ float waves[NW];
+    __shared__ int waves[NW];
     const int b = blockIdx.x / a.touched, nth_page = blockIdx.x % a.touched, h = blockIdx.y * heads_each, last = min(a.cache.heads, h + heads_each);
     const bool values = blockIdx.z != 0;
     const Where w(a, b, nth_page, nth_page == 0 && h == 0 && !values && threadIdx.x == 0);
@@ -396,7 +473,7 @@ static hipError_t launch(const AppendArgs& a, hipStream_t stream) {
         hipLaunchKernelGGL((append_rows_kernel<T, EIGHT>), dim3((unsigned)((items + NW - 1) / NW)), dim3(NT), 0, stream, a);
         return hipGetLastError();
     }
-    const int each = (a.cache.page_tokens * units + NT - 1) / NT;      // 9 at most: pages of 128, 17 units of a head
+    const int rows = NT / rotation_units<4>(a.pairs, a.cache.D), each = (a.cache.page_tokens + rows - 1) / rows;      // 9 at most: pages of 128, 17 units
     if (each <= 2) return launch_pages<T, EIGHT, 2>(a, stream);
     if (each <= 4) return launch_pages<T, EIGHT, 4>(a, stream);
     return launch_pages<T, EIGHT, 9>(a, stream);

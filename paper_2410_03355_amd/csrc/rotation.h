@@ -124,6 +124,24 @@ struct RotationUnit {
             }
         }
     }
+    // The same in the values' own type, for later.
+    __device__ __forceinline__ void load_as(const T* x, T a[NP], T b[NP]) const {
+        if constexpr (WIDE) {
+            typedef typename Vec<T, NP>::type V;
+            const V p = *reinterpret_cast<const V*>(x + o1), q = *reinterpret_cast<const V*>(x + o2);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                a[i] = inter ? (2 * i < NP ? p[2 * i % NP] : q[2 * i % NP]) : p[i];
+                b[i] = inter ? (2 * i < NP ? p[(2 * i + 1) % NP] : q[(2 * i + 1) % NP]) : q[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                a[i] = i < n1 ? x[inter ? o1 + 2 * i : o1 + i] : (T)0.f;
+                b[i] = i < n2 ? x[inter ? o1 + 2 * i + 1 : o2 + i] : (T)0.f;
+            }
+        }
+    }
     __device__ __forceinline__ void turn(float a[NP], float b[NP]) const {
         if (!turned) return;
 #pragma unroll
