@@ -20,6 +20,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "cache_args.h"
 #include "device_utils.h"
@@ -31,7 +32,7 @@ namespace lantern {
 constexpr int MOST_ROWS = LANTERN_MAX_TREE + 1;   // of a sequence
 // Of the lambdas: into their one caller before anything else is done with them, so that what they are handed stays in registers.
 #define INLINE __attribute__((always_inline))
-constexpr float LAZY = 8.f;      // a row's maximum moves up only when a score passes it by 2^8: weights stay under 2^8
+constexpr float LAZY = 8.f;      // a row's maximum moves up only when a score passes it by 8: weights stay under 2^8
 
 struct F32x8 {
     float x[8];
@@ -167,8 +168,10 @@ struct Rows {
     }
 
     // Scores of 32 tokens -> weights.  f > 0: the scores' scale in this lane; vs: what the weights are multiplied by for the second product.
-    // Tokens that are not seen have a score of -inf.
-    __device__ __forceinline__ void weigh(const f32x4 (&s)[QT][2], float f, float vs, Operand (&p)[QT]) {
+    // Tokens that are not seen have a score of -inf.  EARLIER: there are weights that have been summed and wait for the second product.  The
+    // maximum is a whole number, upwards: a step of it is a power of two, by which earlier weights, bf16 ones too, are moved exactly.
+    template <bool EARLIER>
+    __device__ __forceinline__ void weigh(const f32x4 (&s)[QT][2], float f, float vs, Operand (&p)[QT], Operand (&earlier)[QT]) {
         float top[QT];
         bool up = false;
 #pragma unroll
@@ -182,12 +185,16 @@ struct Rows {
         if (__any(up)) {
 #pragma unroll
             for (int qt = 0; qt < QT; ++qt) {
-                const float to = fmaxf(m[qt], over_groups_max(top[qt]));
-                const float by = to == m[qt] ? 1.f : __builtin_amdgcn_exp2f(m[qt] - to);
+                const float to = fmaxf(m[qt], ceilf(over_groups_max(top[qt])));
+                const float by = to == m[qt] ? 1.f : ldexpf(1.f, (int)fmaxf(m[qt] - to, -1000.f));
                 m[qt] = to;
                 sums[qt] *= by;
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) o[qt][dt] *= by;
+                if constexpr (EARLIER) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) set(earlier[qt], j, get(earlier[qt], j) * by);
+                }
             }
         }
         const bool scaled = __any(vs != 1.f);
@@ -636,8 +643,8 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
         wave_sync();
         ask_values(tile, at);
         Operand weights[HALVES][QT];
-#pragma unroll
-        for (int half = 0; half < HALVES; ++half) {
+        auto weigh_half = [&](auto of) INLINE {
+            constexpr int half = of;
             scores(place, half);
             if ((tile + 1) * TOKENS > length) {
 #pragma unroll
@@ -646,8 +653,10 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
                     for (int j = 0; j < 8; ++j)
                         if (8 * half + j >= keep) s[qt][j / 4][j % 4] = neg_inf_f();
             }
-            mine.weigh(s, f, vs, weights[half]);
-        }
+            mine.template weigh<half != 0>(s, f, vs, weights[half], weights[0]);
+        };
+        weigh_half(std::integral_constant<int, 0>());
+        if constexpr (HALVES == 2) weigh_half(std::integral_constant<int, 1>());
         wave_sync();
         put_values(place, tile);
         wave_sync();
@@ -699,7 +708,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
                     if (!(vis[qt] >> j & 1)) s[qt][j / 4][j % 4] = neg_inf_f();
-            mine.weigh(s, a.scale < FLT_MIN ? FLT_MIN : a.scale, 1.f, p);
+            mine.template weigh<false>(s, a.scale < FLT_MIN ? FLT_MIN : a.scale, 1.f, p, p);
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
                 const Operand v = load8(staged + (dt * 16 + col) * ROW + g * CH + half * 8, true);

@@ -84,6 +84,18 @@ def test_large_scores_and_other_scales(lantern_gpu, dtype):
 
 @pytest.mark.parametrize("eight", [True, False])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D,page,M,lengths,by", [(64, 64, 60, (640, 200), 4), (64, 16, 0, (640, 1000, 63), 8), (128, 128, 20, (700, 65), 8),
+                                                 (32, 32, 9, (1200,), 16), (96, 64, 40, (400,), 64)])
+def test_maxima_that_rise_along_a_sequence(lantern_gpu, eight, dtype, D, page, M, lengths, by):
+    """Scores far apart: a row's largest comes up anywhere in a tile of tokens, after weights that are still to be used."""
+    q, *rest = _case(D + by, len(lengths), M, 2, 2, D, page, eight, dtype, lengths)
+    case = (q * by, *rest)
+    want, bound = ref.attend(*case)
+    _check(_gpu(lantern_gpu, *case), want, bound)
+
+
+@pytest.mark.parametrize("eight", [True, False])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_rows_that_are_not_there(lantern_gpu, eight, dtype):
     """Candidates with a parent out of range, and those behind them, have zero rows and are seen by nobody, whatever they hold."""
     case = list(_case(6, 3, 20, 2, 1, 64, 64, eight, dtype, (70, 0, -1)))
