@@ -915,9 +915,30 @@ hipError_t launch_attend_trees(const AttendArgs& a, int dtype, int row_group, hi
     return eight ? launch_width<bf16, true>(a, row_group, stream) : launch_width<bf16, false>(a, row_group, stream);
 }
 
-hipError_t prepare_attend(int, const lantern_cache&) {
+template <typename T, bool EIGHT, int D>
+static hipError_t prepare_rows() {
+    const hipError_t e = allow_lds<attend_trees_kernel<T, EIGHT, D, 1>>(Shared<T, EIGHT, D, 1>::bytes(MOST_ROWS));
+    return e != hipSuccess ? e : allow_lds<attend_trees_kernel<T, EIGHT, D, 2>>(Shared<T, EIGHT, D, 2>::bytes(MOST_ROWS));
+}
+
+template <typename T, bool EIGHT>
+static hipError_t prepare_width(int D) {
+    switch (D) {
+        case 32: return prepare_rows<T, EIGHT, 32>();
+        case 64: return prepare_rows<T, EIGHT, 64>();
+        case 96: return prepare_rows<T, EIGHT, 96>();
+        case 128: return prepare_rows<T, EIGHT, 128>();
+    }
+    return hipSuccess;      // a cache that is not read here
+}
+
+hipError_t prepare_attend(int dtype, const lantern_cache& c) {
     hipFuncAttributes attr;   // the runtime loads all of a file's kernels together
-    return hipFuncGetAttributes(&attr, reinterpret_cast<const void*>(&attend_join_kernel<bf16>));
+    const hipError_t e = hipFuncGetAttributes(&attr, reinterpret_cast<const void*>(&attend_join_kernel<bf16>));
+    if (e != hipSuccess) return e;
+    const bool eight = c.dtype == LANTERN_E4M3;
+    if (dtype == LANTERN_F32) return eight ? prepare_width<float, true>(c.D) : prepare_width<float, false>(c.D);
+    return eight ? prepare_width<bf16, true>(c.D) : prepare_width<bf16, false>(c.D);
 }
 
 }  // namespace lantern

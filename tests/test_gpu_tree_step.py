@@ -118,6 +118,31 @@ def test_captured_step_replays(lantern_gpu):
         assert torch.equal(replayed.lengths, eager.lengths)
 
 
+@pytest.mark.parametrize("dtype,eight,width,rows", [(torch.float32, True, 128, 3), (torch.float32, False, 96, 40), (torch.bfloat16, True, 128, 40)])
+def test_wide_heads_captured_on_their_first_call(lantern_gpu, dtype, eight, width, rows):
+    """prepare_cache before the capture is all that heads need whose tiles take more than 64 KiB of LDS."""
+    gen = torch.Generator().manual_seed(rows)
+    lengths = [700, 0]
+    cache, table = ref.filled_cache(gen, lengths, 1, width, 32, eight)
+    dev, tab = ref.on_gpu(cache), table.cuda()
+    n = torch.tensor(lengths, dtype=torch.int32).cuda()
+    lantern_gpu.prepare_cache(dtype, dev)
+    q, k, v = (ref.normal(gen, 2, rows, 1, width).to(dtype).cuda() for _ in range(3))
+    parent = torch.from_numpy(trees.random_trees(np.random.default_rng(5), 2, rows - 1).reshape(-1)).int().cuda()
+    need = lantern_gpu.attend_trees_workspace_bytes(dtype, 2, rows - 1, 1, dev, tab.shape[1])
+    space = torch.empty(need, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = lantern_gpu.attend_trees(q, k, v, parent, dev, tab, n, workspace=space)
+    for turn in range(3):
+        q.copy_(ref.normal(gen, 2, rows, 1, width))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, lantern_gpu.attend_trees(q, k, v, parent, dev, tab, n))
+
+
 def test_two_graphs_with_workspaces_of_their_own(lantern_gpu):
     """Split sequences captured twice, replayed at the same time on two streams."""
     gen = torch.Generator().manual_seed(3)
