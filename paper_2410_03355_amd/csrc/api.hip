@@ -577,7 +577,7 @@ int lantern_attend_trees(const void* q, const int64_t* q_strides, const void* k,
     a.by_tiles = lantern::Divisor(plan.row_tiles);
     a.by_heads = lantern::Divisor(cache->heads);
     a.by_group = lantern::Divisor(a.group);
-    const hipError_t e = lantern::launch_attend_trees(a, dtype, plan.row_group, static_cast<hipStream_t>(hip_stream));
+    const hipError_t e = lantern::launch_attend_trees(a, dtype, plan.row_group, plan.abreast, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? LANTERN_OK : LANTERN_E_DEVICE;
 }
 

@@ -12,7 +12,7 @@
 // tile t, lane group g ends with the scores of tokens CH * g .. CH * g + CH - 1, and those are the ones it has to hold of P, so
 // no value changes its lane.  Values are cached as [D][token] for the same reason: CH tokens of one element are 16 bytes.
 //
-// The four wavefronts of a workgroup take every fourth tile of tokens each and join through LDS; where sequences, heads and
+// The four wavefronts of a workgroup take the same rows, or two sets of them, and every fourth (second) tile of tokens each, and join through LDS; where sequences, heads and
 // row tiles are too few to fill the device a sequence is split over workgroups as well, whose parts a second kernel joins.
 #include <hip/hip_runtime.h>
 #include <float.h>
@@ -83,6 +83,26 @@ __device__ __forceinline__ F32x8 from_bf16<float>(u32x4 w) {
 }
 __device__ __forceinline__ void set(bf16x8& f, int i, float x) { f[i] = (bf16)x; }
 __device__ __forceinline__ void set(F32x8& f, int i, float x) { f.x[i] = x; }
+
+__device__ __forceinline__ bf16 element_of(const bf16x8& f, int i) { return f[i]; }
+__device__ __forceinline__ float element_of(const F32x8& f, int i) { return f.x[i]; }
+__device__ __forceinline__ bf16x8 zeros(const bf16x8&) { return __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u}); }
+__device__ __forceinline__ F32x8 zeros(const F32x8&) { return F32x8{}; }
+// All eight finite: no exponent of ones only.
+__device__ __forceinline__ bool finite(const bf16x8& f) {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    const u32x4 w = __builtin_bit_cast(u32x4, f);
+    u16x2 top = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w[i] & 0x7FFF7FFFu));
+    return max(top[0], top[1]) < 0x7F80u;
+}
+__device__ __forceinline__ bool finite(const F32x8& f) {
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f.x[i]) & 0x7FFFFFFFu);
+    return top < 0x7F800000u;
+}
 
 __device__ __forceinline__ float get(const bf16x8& f, int i) { return (float)f[i]; }
 __device__ __forceinline__ float get(const F32x8& f, int i) { return f.x[i]; }
@@ -275,8 +295,9 @@ struct Parts {
     __device__ __forceinline__ int count(int tiles) const { return tiles <= size ? 1 : (int)((unsigned)(tiles + size - 1) / (unsigned)size); }
 };
 
-// Four wavefronts take the same QT * 16 rows, each through every fourth tile of a sequence's cached tokens.
-template <typename T, bool EIGHT, int D, int QT>
+// ABREAST wavefronts of a workgroup take QT * 16 rows each, side by side; the TEAMS that there are of such take a sequence's tiles of cached
+// tokens in turn.
+template <typename T, bool EIGHT, int D, int QT, int ABREAST>
 __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_trees_kernel(AttendArgs a) {
     typedef Rows<T, D, QT> Mine;
     typedef Tile<EIGHT, D> Tokens;
@@ -284,6 +305,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
     typedef typename Frag<T>::type Operand;
     constexpr int CH = Tokens::CH, TOKENS = Tokens::TOKENS, STEPS = D / 32, DT = D / 16, SIZE = Tokens::SIZE, HALVES = CH / 8;
     constexpr int ROW = Lds::OWN_VROW, PARTS = Tokens::PARTS;
+    constexpr int TEAMS = NW / ABREAST;
     constexpr int PER = Tokens::CHUNKS / WAVE;      // chunks of a tile to a lane
     extern __shared__ __attribute__((aligned(16))) char shared[];
     __shared__ float wave_m[NW][16 * QT], wave_l[NW][16 * QT];
@@ -297,7 +319,9 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
     int *const jump = reinterpret_cast<int*>(present + words), *const lost = jump + rows_of;
     // The row tiles of one part of a sequence and head read the same tokens: they get numbers 8 apart, which one XCD serves.
     const int chunk = a.by_tiles.of(blockIdx.x >> 3);
-    const int item = chunk * 8 + (int)(blockIdx.x & 7), first_row = ((int)(blockIdx.x >> 3) - chunk * a.row_tiles) * 16 * QT;
+    const int item = chunk * 8 + (int)(blockIdx.x & 7);
+    const int beside = wave % ABREAST, team = wave / ABREAST;
+    const int group_row = ((int)(blockIdx.x >> 3) - chunk * a.row_tiles) * (16 * QT * ABREAST), first_row = group_row + beside * 16 * QT;
     const int part = a.by_heads.of(item), h = item - part * heads;
     if (part >= a.parts) return;
     int b = part, nth = 0, size = INT_MAX;      // the sequence, its part, and how many tiles that has
@@ -325,7 +349,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
     const bool absent = told < 0, too_long = (int64_t)told > (int64_t)a.width << a.page_shift;
     const int length = absent || too_long ? 0 : told;
     const int tiles = (length + TOKENS - 1) / TOKENS;
-    const int begin = whole ? wave : nth * size + wave, end = whole ? tiles : min(tiles, (nth + 1) * size);
+    const int begin = (whole ? 0 : nth * size) + team, end = ABREAST > 1 && first_row >= R ? 0 : whole ? tiles : min(tiles, (nth + 1) * size);
     const bool has_tree = whole || (nth + 1) * size >= tiles;
 
     // ---- the rows: B of the first product
@@ -347,7 +371,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
     mine.begin();
 
     // ---- where the cached tokens are
-    const int last = begin < end ? begin + (end - 1 - begin) / NW * NW : begin;      // this wavefront's last tile
+    const int last = begin < end ? begin + (end - 1 - begin) / TEAMS * TEAMS : begin;      // this wavefront's last tile
     const int32_t* const table = a.table + (int64_t)b * a.width;
     const unsigned page_bytes = (unsigned)heads * page * D * SIZE;      // 65535 heads at most: under 2^31
     const char* const kbase = static_cast<const char*>(a.cache.k) + (int64_t)h * page * D * SIZE;
@@ -461,7 +485,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
         }
         return s;
     };
-    auto tile_after = [&](int tile) INLINE { return min(tile + NW, last); };
+    auto tile_after = [&](int tile) INLINE { return min(tile + TEAMS, last); };
     int ids = ask_ids(begin);
     Scales scales = {1.f, 1.f, false};
 
@@ -475,8 +499,8 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
         *bad = 1;
         return 0;
     };
-    // Own rows on their way to LDS, 8 elements to a thread: keys in the order of the product's rows, values turned over with those that are not
-    // finite taken out.  Neighbouring threads have neighbouring elements of a key, and the same elements of neighbouring values: what
+    // Own rows on their way to LDS, 8 elements to a thread: keys in the order of the product's rows, values turned over; where one is not
+    // finite, such values are taken out by another pass.  Neighbouring threads have neighbouring elements of a key, and the same elements of neighbouring values: what
     // they write then lies next to each other.
     constexpr int OWN = TOKENS * (D / 8), OWN_PER = (OWN + NT - 1) / NT;
     struct Taken {
@@ -498,15 +522,22 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
         for (int n = 0; n < OWN_PER; ++n) {
             const int e = min((int)threadIdx.x + n * NT, OWN - 1), i = e % TOKENS, d = e / TOKENS * 8;
             *reinterpret_cast<Operand*>(own_keys + Tokens::row_of(e / (D / 8)) * Lds::OWN_KROW + e % (D / 8) * 8 * (int)sizeof(T)) = t.k[n];
+            const Operand v = base + i < rows_of ? t.v[n] : zeros(t.v[n]);
+            odd |= !finite(v);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float x = base + i < rows_of ? get(t.v[n], j) : 0.f;
-                const bool fine = fabsf(x) < __builtin_huge_valf();
-                odd |= !fine;
-                staged[(d + j) * ROW + i] = (T)(fine ? x : 0.f);
-            }
+            for (int j = 0; j < 8; ++j) staged[(d + j) * ROW + i] = element_of(v, j);
         }
         return odd;
+    };
+    auto clean = [&]() INLINE {      // seldom: 0 for what is not finite of this thread's values
+#pragma unroll 1
+        for (int e = threadIdx.x; e < OWN; e += NT)
+#pragma unroll 1
+            for (int j = 0; j < 8; ++j) {
+                T& x = staged[(e / TOKENS * 8 + j) * ROW + e % TOKENS];
+                if (!(fabsf((float)x) < __builtin_huge_valf())) x = (T)0.f;
+            }
+        __syncthreads();
     };
     Taken taken;
     const int i = threadIdx.x;
@@ -573,6 +604,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
         const uint64_t alive = __ballot(i < rows_of && !bad);
         if (lane < 2 && 2 * wave + lane < words) present[2 * wave + lane] = (unsigned)(alive >> 32 * lane);
         odd = __syncthreads_or(odd);
+        if (odd) clean();
     }
 
     // ---- cached tokens, a half of a tile (8 tokens of every lane group) at a time
@@ -626,7 +658,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
         }
     };
     char* const place = shared + wave * Lds::TILE;
-    for (int tile = begin; tile < end; tile += NW) {
+    for (int tile = begin; tile < end; tile += TEAMS) {
         float f = a.scale * scales.k, vs = scales.v, two = 1.f;
         f = f < FLT_MIN ? FLT_MIN : f;                   // -inf * f stays -inf
         if (scales.bad) f = __builtin_nanf("");          // what the page should have held is not known: the rows become NaN
@@ -682,10 +714,11 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
             taken = a.wide ? take(base, true) : take(base, false);
             __syncthreads();
             odd = __syncthreads_or(stage(taken, base));
+            if (odd) clean();
         }
 #pragma unroll 1
         for (int half = 0; half < HALVES; ++half, ++turn) {
-            if (turn % NW != NW - 1 - wave) continue;
+            if (turn % TEAMS != TEAMS - 1 - team || (ABREAST > 1 && first_row >= R)) continue;
             const int at = base + g * CH + half * 8;      // the first of this lane group's 8
             unsigned vis[QT];
 #pragma unroll
@@ -759,23 +792,23 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
     }
     __syncthreads();
     const int64_t rows_all = (int64_t)a.parts * heads * R;
-    constexpr int UNITS = ROWS * (D / 4);
+    constexpr int UNITS = ABREAST * ROWS * (D / 4);
 #pragma unroll
     for (int n = 0; n < (UNITS + NT - 1) / NT; ++n) {
-        const int e = threadIdx.x + n * NT, rr = e / (D / 4), d = e % (D / 4) * 4, row = first_row + rr;
+        const int e = threadIdx.x + n * NT, d = e % (D / 4) * 4, rr = e / (D / 4) % ROWS, with = e / (D / 4) / ROWS, row = group_row + e / (D / 4);
         if (e >= UNITS || row >= R) continue;
-        float m[NW], high = neg_inf_f(), all = 0.f;
+        float m[TEAMS], high = neg_inf_f(), all = 0.f;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            m[w] = wave_m[w][rr];
+        for (int w = 0; w < TEAMS; ++w) {
+            m[w] = wave_m[w * ABREAST + with][rr];
             high = fmaxf(high, m[w]);
         }
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < NW; ++w) {
+        for (int w = 0; w < TEAMS; ++w) {
             const float by = m[w] == high ? 1.f : __builtin_amdgcn_exp2f(m[w] - high);
-            sum += by * *reinterpret_cast<const f32x4*>(&joined[w * PART + rr * (D + 4) + d]);
-            all += by * wave_l[w][rr];
+            sum += by * *reinterpret_cast<const f32x4*>(&joined[(w * ABREAST + with) * PART + rr * (D + 4) + d]);
+            all += by * wave_l[w * ABREAST + with][rr];
         }
         const bool none = all == 0.f;       // nothing seen with a weight, or no row
         if (whole) {
@@ -863,13 +896,18 @@ AttendPlan plan_attend(int dtype, int B, int M, int q_heads, const lantern_cache
     AttendPlan p;
     const int64_t R = (int64_t)(M + 1) * (q_heads / c.heads);
     // Tiles of 16 rows that a wavefront takes together: each conversion of a tile of tokens serves all of them.  Four (D <= 64, 246 registers)
-    // are no faster where they have all their use: 64 trees of 61 rows 55.1 us against 53.8 with two, one tree 14.8 against 11.3.
+    // were no faster where they had all their use: 64 trees of 61 rows 55.1 us against 53.8 with two, one tree 14.8 against 11.3.
     p.row_group = R <= 16 ? 1 : 2;
-    p.row_tiles = (int)((R + 16 * p.row_group - 1) / (16 * p.row_group));
+    const int64_t room = dtype == LANTERN_BF16 && c.D <= 64 ? 768 : 512, tiles = (R + 16 * p.row_group - 1) / (16 * p.row_group);
+    // Where workgroups of one set of such tiles are more than fit at once, two wavefronts take two sets side by side: half the workgroups,
+    // which bring own rows, tree and arguments for twice the work.  20 heads, trees of 61 rows: 64 sequences 45.5 us against 52.5, 39 30.5
+    // against 32.9, 20 21.3 against 22.8, but one 15.4 against 11.1.  fp32 is bound by its products and loses (32 sequences 97 against 87).
+    p.abreast = dtype == LANTERN_BF16 && tiles > 1 && B * c.heads * tiles > room ? 2 : 1;
+    p.row_tiles = (int)((tiles + p.abreast - 1) / p.abreast);
     // Where sequences, heads and row tiles make fewer workgroups than fit the 256 CUs at once (two or three to a CU), sequences are cut:
     // into parts of two tiles to a wavefront at least.
     const int64_t groups = (int64_t)c.heads * p.row_tiles, tokens = (int64_t)width * c.page_tokens;
-    const int64_t room = dtype == LANTERN_BF16 && c.D <= 64 ? 768 : 512, tile = c.dtype == LANTERN_E4M3 ? 64 : 32;
+    const int64_t tile = c.dtype == LANTERN_E4M3 ? 64 : 32;
     const int64_t useful = std::max<int64_t>(1, tokens / (tile * NW * 2));
     const int64_t parts = std::min(room / groups, B * useful);
     p.parts = (int)(parts >= 2 * (int64_t)B ? parts : B);
@@ -877,15 +915,15 @@ AttendPlan plan_attend(int dtype, int B, int M, int q_heads, const lantern_cache
     return p;
 }
 
-template <typename T, bool EIGHT, int D, int QT>
+template <typename T, bool EIGHT, int D, int QT, int ABREAST>
 static hipError_t launch(const AttendArgs& a, hipStream_t stream) {
-    hipError_t e = allow_lds<attend_trees_kernel<T, EIGHT, D, QT>>(Shared<T, EIGHT, D, QT>::bytes(MOST_ROWS));
+    hipError_t e = allow_lds<attend_trees_kernel<T, EIGHT, D, QT, ABREAST>>(Shared<T, EIGHT, D, QT>::bytes(MOST_ROWS));
     if (e != hipSuccess) return e;
     const int64_t items = (int64_t)a.parts * a.cache.heads;
     const int R = (a.M + 1) * a.group;
     const int blocks = (int)((items + 7) / 8 * 8 * a.row_tiles);
     const int lds = Shared<T, EIGHT, D, QT>::bytes(a.M + 1);
-    hipLaunchKernelGGL((attend_trees_kernel<T, EIGHT, D, QT>), dim3(blocks), dim3(NT), lds, stream, a);
+    hipLaunchKernelGGL((attend_trees_kernel<T, EIGHT, D, QT, ABREAST>), dim3(blocks), dim3(NT), lds, stream, a);
     e = hipGetLastError();
     if (e != hipSuccess || a.parts == a.B) return e;
     hipLaunchKernelGGL((attend_join_kernel<T>), dim3(a.B, a.cache.heads, (R * (D / 4) + WAVE - 1) / WAVE), dim3(NT), 0, stream, a, (int)Tile<EIGHT, D>::TOKENS);
@@ -893,32 +931,39 @@ static hipError_t launch(const AttendArgs& a, hipStream_t stream) {
 }
 
 template <typename T, bool EIGHT, int D>
-static hipError_t launch_rows(const AttendArgs& a, int row_group, hipStream_t stream) {
-    if (row_group == 1) return launch<T, EIGHT, D, 1>(a, stream);
-    return launch<T, EIGHT, D, 2>(a, stream);
+static hipError_t launch_rows(const AttendArgs& a, int row_group, int abreast, hipStream_t stream) {
+    if (row_group == 1) return launch<T, EIGHT, D, 1, 1>(a, stream);
+    if constexpr (sizeof(T) == 2) {
+        if (abreast == 2) return launch<T, EIGHT, D, 2, 2>(a, stream);
+    }
+    return launch<T, EIGHT, D, 2, 1>(a, stream);
 }
 
 template <typename T, bool EIGHT>
-static hipError_t launch_width(const AttendArgs& a, int row_group, hipStream_t stream) {
+static hipError_t launch_width(const AttendArgs& a, int row_group, int abreast, hipStream_t stream) {
     switch (a.cache.D) {
-        case 32: return launch_rows<T, EIGHT, 32>(a, row_group, stream);
-        case 64: return launch_rows<T, EIGHT, 64>(a, row_group, stream);
-        case 96: return launch_rows<T, EIGHT, 96>(a, row_group, stream);
-        case 128: return launch_rows<T, EIGHT, 128>(a, row_group, stream);
+        case 32: return launch_rows<T, EIGHT, 32>(a, row_group, abreast, stream);
+        case 64: return launch_rows<T, EIGHT, 64>(a, row_group, abreast, stream);
+        case 96: return launch_rows<T, EIGHT, 96>(a, row_group, abreast, stream);
+        case 128: return launch_rows<T, EIGHT, 128>(a, row_group, abreast, stream);
     }
     return hipErrorInvalidValue;
 }
 
-hipError_t launch_attend_trees(const AttendArgs& a, int dtype, int row_group, hipStream_t stream) {
+hipError_t launch_attend_trees(const AttendArgs& a, int dtype, int row_group, int abreast, hipStream_t stream) {
     const bool eight = a.cache.dtype == LANTERN_E4M3;
-    if (dtype == LANTERN_F32) return eight ? launch_width<float, true>(a, row_group, stream) : launch_width<float, false>(a, row_group, stream);
-    return eight ? launch_width<bf16, true>(a, row_group, stream) : launch_width<bf16, false>(a, row_group, stream);
+    if (dtype == LANTERN_F32) return eight ? launch_width<float, true>(a, row_group, abreast, stream) : launch_width<float, false>(a, row_group, abreast, stream);
+    return eight ? launch_width<bf16, true>(a, row_group, abreast, stream) : launch_width<bf16, false>(a, row_group, abreast, stream);
 }
 
 template <typename T, bool EIGHT, int D>
 static hipError_t prepare_rows() {
-    const hipError_t e = allow_lds<attend_trees_kernel<T, EIGHT, D, 1>>(Shared<T, EIGHT, D, 1>::bytes(MOST_ROWS));
-    return e != hipSuccess ? e : allow_lds<attend_trees_kernel<T, EIGHT, D, 2>>(Shared<T, EIGHT, D, 2>::bytes(MOST_ROWS));
+    hipError_t e = allow_lds<attend_trees_kernel<T, EIGHT, D, 1, 1>>(Shared<T, EIGHT, D, 1>::bytes(MOST_ROWS));
+    if (e == hipSuccess) e = allow_lds<attend_trees_kernel<T, EIGHT, D, 2, 1>>(Shared<T, EIGHT, D, 2>::bytes(MOST_ROWS));
+    if constexpr (sizeof(T) == 2) {
+        if (e == hipSuccess) e = allow_lds<attend_trees_kernel<T, EIGHT, D, 2, 2>>(Shared<T, EIGHT, D, 2>::bytes(MOST_ROWS));
+    }
+    return e;
 }
 
 template <typename T, bool EIGHT>

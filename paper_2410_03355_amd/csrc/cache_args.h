@@ -60,21 +60,21 @@ struct AttendArgs {
     Strided sq, sk, sv;
     float scale;            // of the scores, times log2(e)
     void* out;              // [B, M + 1, q_heads, D]
-    int parts, row_tiles;   // parts of all sequences, B or more
+    int parts, row_tiles;   // parts of all sequences, B or more; sets of rows, one to a workgroup
     double per_part;        // 1 / (parts - B), a little more
     float* part;            // where they are more: outputs [parts, heads, rows, D], then maxima and sums [parts, heads, rows]
     Divisor by_tiles, by_heads, by_group;
 };
 
 struct AttendPlan {
-    int parts, row_tiles, row_group;
+    int parts, row_tiles, row_group, abreast;
     size_t workspace;
 };
 AttendPlan plan_attend(int dtype, int B, int M, int q_heads, const lantern_cache& c, int width);
 
 hipError_t launch_rotate_axes(const RotateArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_append_cache(const AppendArgs& a, int dtype, hipStream_t stream);
-hipError_t launch_attend_trees(const AttendArgs& a, int dtype, int row_group, hipStream_t stream);
+hipError_t launch_attend_trees(const AttendArgs& a, int dtype, int row_group, int abreast, hipStream_t stream);
 hipError_t prepare_rotate(int dtype);
 hipError_t prepare_append(int dtype, const lantern_cache& c);
 hipError_t prepare_attend(int dtype, const lantern_cache& c);

@@ -95,6 +95,23 @@ def test_maxima_that_rise_along_a_sequence(lantern_gpu, eight, dtype, D, page, M
 
 
 @pytest.mark.parametrize("eight", [True, False])
+@pytest.mark.parametrize("B,G,Hk,M,D,page", [(20, 1, 20, 32, 32, 32), (23, 2, 12, 40, 64, 64), (10, 1, 20, 70, 128, 64), (25, 3, 16, 10, 96, 128)])
+def test_more_sequences_than_fit_at_once(lantern_gpu, eight, B, G, Hk, M, D, page):
+    """Sets of rows side by side in a workgroup, the last one empty or not; the last row, a leaf, has a value that is infinite."""
+    lengths = [(0, 1, 65, 130, -1, 40)[b % 6] for b in range(B)]
+    q, k, v, parent, cache, table, n = _case(B, B, M, G, Hk, D, page, eight, torch.bfloat16, lengths)
+    assert lantern_gpu.attend_trees_workspace_bytes(torch.bfloat16, B, M, G * Hk, ref.on_gpu(cache), table.shape[1]) == 0
+    want, bound = ref.attend(q, k, v, parent, cache, table, n)
+    odd = v.clone()
+    odd[:, -1, :, 0] = math.inf
+    got = _gpu(lantern_gpu, q, k, odd, parent, cache, table, n)
+    _check(got[:, :-1], want[:, :-1], bound[:, :-1])
+    there = n >= 0
+    assert not bool(got[there][:, -1, :, 0].isfinite().any())
+    _check(got[there][:, -1, :, 1:], want[there][:, -1, :, 1:], bound[there][:, -1, :, 1:])
+
+
+@pytest.mark.parametrize("eight", [True, False])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_rows_that_are_not_there(lantern_gpu, eight, dtype):
     """Candidates with a parent out of range, and those behind them, have zero rows and are seen by nobody, whatever they hold."""
