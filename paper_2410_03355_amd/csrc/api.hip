@@ -572,7 +572,9 @@ int lantern_attend_trees(const void* q, const int64_t* q_strides, const void* k,
     a.out = out;
     a.part = static_cast<float*>(workspace);
     a.parts = plan.parts;
+    a.cut = a.part ? reinterpret_cast<int2*>(a.part + (size_t)plan.parts * cache->heads * (M + 1) * a.group * (cache->D + 2)) : nullptr;
     a.per_part = plan.parts > B ? (1.0 + 1e-12) / (plan.parts - B) : 0.0;
+    a.per_all = (1.0 - 1e-12) / (4.0 * plan.parts);
     a.row_tiles = plan.row_tiles;
     a.by_tiles = lantern::Divisor(plan.row_tiles);
     a.by_heads = lantern::Divisor(cache->heads);

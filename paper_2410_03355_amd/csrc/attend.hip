@@ -271,8 +271,9 @@ struct Shared {
 };
 
 // Parts of the B sequences where there are `parts` > B: all are of as many tiles of tokens, the last of a sequence of what is left, and
-// a sequence has one at least.  With tiles T_b and size = T / (parts - B), sum ceil(T_b / size) <= parts.  Every wavefront finds its
-// part from the lengths by itself.
+// a sequence has one at least.  With tiles T_b and size = T / (parts - B), sum ceil(T_b / size) <= parts; the least such size lies between
+// that and T / parts, and a wavefront that has a sequence to a lane finds it by halves (4 trees behind 2000 to 16001 tokens: 56 tiles instead
+// of 72).  Every wavefront finds its part from the lengths by itself.
 struct Parts {
     int size;      // tiles
     __device__ __forceinline__ static int tiles_of(const AttendArgs& a, int b, int tokens) {
@@ -289,8 +290,19 @@ struct Parts {
         }
         low = __builtin_amdgcn_readlane(wave_scan_i<OpSum>(low, 0), WAVE - 1);
         high = __builtin_amdgcn_readlane(wave_scan_i<OpSum>(high, 0), WAVE - 1);
-        const int most = (int)(((double)high * 65536.0 + (double)low) * a.per_part) + 1;      // per_part: 1 / (parts - B), a little more
-        size = (most + NW - 1) / NW * NW;
+        const double all = (double)high * 65536.0 + (double)low;
+        size = ((int)(all * a.per_part) + NW) / NW * NW;      // per_part: 1 / (parts - B), a little more
+        if (a.B <= WAVE) {
+            const int mine = tiles_of(a, lane, tokens), low_rounds = max(1, (int)(all * a.per_all));      // per_all: 1 / (parts * NW), a little less
+            for (int from = low_rounds, to = size / NW; from < to;) {
+                const int mid = (from + to) / 2;
+                size = mid * NW;
+                const int n = __builtin_amdgcn_readlane(wave_scan_i<OpSum>(lane < a.B ? count(mine) : 0, 0), WAVE - 1);
+                if (n <= a.parts) to = mid;
+                else from = mid + 1;
+                size = to * NW;
+            }
+        }
     }
     __device__ __forceinline__ int count(int tiles) const { return tiles <= size ? 1 : (int)((unsigned)(tiles + size - 1) / (unsigned)size); }
 };
@@ -338,7 +350,9 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
                 const int at = __ffsll((long long)mine) - 1;
                 b = base + at;
                 nth = part - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(n, at));
-                whole = __builtin_amdgcn_readlane(n, at) == 1;
+                const int of = __builtin_amdgcn_readlane(n, at);
+                whole = of == 1;
+                if (nth == 0 && h == 0 && group_row == 0 && threadIdx.x == 0) a.cut[b] = make_int2(part, of);      // for the join
                 break;
             }
             before = __builtin_amdgcn_readlane(upto, WAVE - 1);
@@ -833,19 +847,12 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 && D <= 64 ? 3 : 2) void attend_
 // The parts of a sequence's rows joined.  A workgroup takes 64 pieces of 4 elements of the rows of one sequence and head, a piece to a lane,
 // and its wavefronts every fourth part.  Sequences of one part have been written already.
 template <typename T>
-__global__ __launch_bounds__(NT) void attend_join_kernel(AttendArgs a, int tokens) {
+__global__ __launch_bounds__(NT) void attend_join_kernel(AttendArgs a) {
     __shared__ f32x4 sums[NW][WAVE];
     __shared__ float highs[NW][WAVE], alls[NW][WAVE];
     const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), heads = a.cache.heads, D = a.cache.D, rows_of = a.M + 1, R = rows_of * a.group;
     const int b = blockIdx.x, h = blockIdx.y;
-    const Parts parts(a, tokens);
-    int first = 0, n = 0;
-    for (int base = 0; base <= b; base += WAVE) {
-        const int mine = base + lane < a.B ? parts.count(Parts::tiles_of(a, base + lane, tokens)) : 0;
-        const int upto = wave_scan_i<OpSum>(mine, 0), at = min(b - base, WAVE - 1);
-        n = __builtin_amdgcn_readlane(mine, at);
-        first += __builtin_amdgcn_readlane(upto, at) - (b - base < WAVE ? n : 0);
-    }
+    const int first = a.cut[b].x, n = a.cut[b].y;
     if (n == 1) return;
     const int64_t rows_all = (int64_t)a.parts * heads * R;
     const float *const pm = a.part + rows_all * D, *const pl = pm + rows_all;
@@ -911,7 +918,7 @@ AttendPlan plan_attend(int dtype, int B, int M, int q_heads, const lantern_cache
     const int64_t useful = std::max<int64_t>(1, tokens / (tile * NW * 2));
     const int64_t parts = std::min(room / groups, B * useful);
     p.parts = (int)(parts >= 2 * (int64_t)B ? parts : B);
-    p.workspace = p.parts == B ? 0 : (size_t)p.parts * c.heads * R * (c.D + 2) * sizeof(float);
+    p.workspace = p.parts == B ? 0 : (size_t)p.parts * c.heads * R * (c.D + 2) * sizeof(float) + B * sizeof(int2);
     return p;
 }
 
@@ -926,7 +933,7 @@ static hipError_t launch(const AttendArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((attend_trees_kernel<T, EIGHT, D, QT, ABREAST>), dim3(blocks), dim3(NT), lds, stream, a);
     e = hipGetLastError();
     if (e != hipSuccess || a.parts == a.B) return e;
-    hipLaunchKernelGGL((attend_join_kernel<T>), dim3(a.B, a.cache.heads, (R * (D / 4) + WAVE - 1) / WAVE), dim3(NT), 0, stream, a, (int)Tile<EIGHT, D>::TOKENS);
+    hipLaunchKernelGGL((attend_join_kernel<T>), dim3(a.B, a.cache.heads, (R * (D / 4) + WAVE - 1) / WAVE), dim3(NT), 0, stream, a);
     return hipGetLastError();
 }
 

@@ -61,8 +61,9 @@ struct AttendArgs {
     float scale;            // of the scores, times log2(e)
     void* out;              // [B, M + 1, q_heads, D]
     int parts, row_tiles;   // parts of all sequences, B or more; sets of rows, one to a workgroup
-    double per_part;        // 1 / (parts - B), a little more
+    double per_part, per_all;   // 1 / (parts - B), a little more; 1 / (4 * parts), a little less
     float* part;            // where they are more: outputs [parts, heads, rows, D], then maxima and sums [parts, heads, rows]
+    int2* cut;              // behind them: a sequence's first part and how many it has
     Divisor by_tiles, by_heads, by_group;
 };
 
