@@ -631,7 +631,7 @@ int lantern_append_cache(const lantern_cache* cache, const int32_t* table, int t
  *            there: its row of the output is zero and no row sees it.
  *   table, table_width, lengths  as in lantern_append_cache; lengths may be 0, and
  *            all rows of a place without a sequence (negative) are zero
- *   scale    of the scores, finite and >= 0
+ *   scale    of the scores, from 0 to FLT_MAX / 2
  *   out      device, [B, M+1, q_heads, D] dense, dtype
  *   workspace  device memory, 256-byte aligned, of at least
  *            lantern_attend_trees_workspace_bytes; owned by the caller, contents
@@ -647,7 +647,8 @@ int lantern_append_cache(const lantern_cache* cache, const int32_t* table, int t
  * are rounded to bfloat16 for the second product, half a step of 2^-8 each.
  * Errors: E_DTYPE, E_SHAPE (B < 0, M < 0, M > LANTERN_MAX_TREE, q_heads not a
  * positive multiple of the cache's heads, table_width < 1 or too many tokens, the
- * cache's limits, scale not finite or negative, more workgroups or rows than INT_MAX),
+ * cache's limits, scale out of its range, 2^24 workgroups, one to a
+ * sequence, key head and 16 rows or more, or rows beyond INT_MAX),
  * E_NULL, E_WORKSPACE, E_DEVICE.  B = 0 does nothing.
  */
 #define LANTERN_MAX_TREE 255

@@ -796,10 +796,31 @@ def _rotation_args(positions, freqs, sections, interleaved, rows: int):
     return _Rotation(positions.data_ptr(), freqs.data_ptr(), len(sections), (ctypes.c_int * MAX_AXES)(*sections), int(bool(interleaved)))
 
 
+def _wants_gradients(*tensors) -> bool:
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
+class _Turned(torch.autograd.Function):
+    """rotate_axes where gradients are wanted: turning is orthogonal, so theirs is to turn back."""
+
+    @staticmethod
+    def forward(ctx, q, k, positions, freqs, sections, interleaved, inverse):
+        ctx.save_for_backward(positions, freqs)
+        ctx.how = sections, interleaved, inverse
+        return rotate_axes(q, k, positions, freqs, sections, interleaved, inverse)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        sections, interleaved, inverse = ctx.how
+        grads = [g if g is None or g.shape[2] == 1 or g.stride(2) == 1 else g.contiguous() for g in grads]
+        return (*rotate_axes(*grads, *ctx.saved_tensors, sections, interleaved, not inverse), None, None, None, None, None)
+
+
 def rotate_axes(q, k, positions, freqs, sections, interleaved: bool = False, inverse: bool = False, out=None, stream=None):
     """lantern_rotate_axes: q [N, heads, D] and k [N, heads, D] (or None) turned by positions [N, axes]; sections: pairs of
     each axis, freqs [their sum].  Returns (q, k) turned, new tensors or those of `out` (a pair, which may be q and k
-    themselves).  inverse turns back, which is the gradient: it takes the outputs' gradients to the inputs'."""
+    themselves).  inverse turns back, which is the gradient: it takes the outputs' gradients to the inputs'.  Where autograd
+    records q or k that is done in their backward pass (with out or stream such a call is refused; freqs have no gradient)."""
     lib = load()
     if out is None and stream is None:
         got = _marshal.rotate_axes(q, k, positions, freqs, sections, interleaved, inverse)
@@ -809,6 +830,10 @@ def rotate_axes(q, k, positions, freqs, sections, interleaved: bool = False, inv
     for t in ts:
         if t.dim() != 3 or t.shape[0] != q.shape[0] or t.shape[2] != q.shape[2] or t.dtype != q.dtype or (t.shape[2] > 1 and t.stride(2) != 1):
             raise ValueError("q and k must be [N, heads, D] of the same N, D and dtype, with dense heads")
+    if _wants_gradients(*ts, freqs):
+        if out is not None or stream is not None or freqs.requires_grad:
+            raise ValueError("gradients are recorded without out and stream, and freqs have none")
+        return _Turned.apply(q, k, positions, freqs, sections, interleaved, inverse)
     _need_here(stream, *ts, positions, freqs)
     N, _, D = q.shape
     code = _dtype_code(q)
@@ -848,6 +873,8 @@ def append_cache(cache, table, lengths, k, v, positions=None, freqs=None, sectio
         got = _marshal.append_cache(cache, table, lengths, k, v, positions, freqs, sections, interleaved, path, count)
         if got is not None:
             return _checked_status(got, "lantern_append_cache")
+    if _wants_gradients(k, v):
+        raise ValueError("there is no backward pass here: call it under torch.no_grad()")
     c, parts = _cache_args(cache)
     _rows_of_cache(c, k, v)
     B, T = k.shape[:2]
@@ -889,6 +916,8 @@ def attend_trees(q, k, v, parent, cache, table, lengths, scale=None, workspace=N
         got = _marshal.attend_trees(q, k, v, parent, cache, table, lengths, scale, workspace)
         if got is not None:
             return _checked_status(got, "lantern_attend_trees")
+    if _wants_gradients(q, k, v):
+        raise ValueError("there is no backward pass here: call it under torch.no_grad()")
     c, parts = _cache_args(cache)
     _rows_of_cache(c, k, v)
     B, T = k.shape[:2]
@@ -897,6 +926,8 @@ def attend_trees(q, k, v, parent, cache, table, lengths, scale=None, workspace=N
     _table_args(table, lengths, B)
     if parent is not None and (parent.dtype != torch.int32 or parent.numel() != B * (T - 1) or not parent.is_contiguous()):
         raise ValueError("parent must be a contiguous int32 tensor of B*M entries")
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
     _need_here(stream, *parts, table, lengths, q, k, v, parent, workspace)
     code, Hq, width = _dtype_code(q), q.shape[2], table.shape[1]
     need = int(lib.lantern_attend_trees_workspace_bytes(code, B, T - 1, Hq, ctypes.byref(c), width))

@@ -449,7 +449,7 @@ int attend_plan(lantern_dtype dtype, int B, int M, int q_heads, const lantern_ca
     const int64_t group = q_heads / cache->heads;
     if (group * (M + 1) > INT_MAX / 2 || (int64_t)B * q_heads > INT_MAX / (M + 1)) return LANTERN_E_SHAPE;
     *plan = lantern::plan_attend(dtype, B, M, q_heads, *cache, width);
-    return ((int64_t)plan->parts * cache->heads + 8) * plan->row_tiles > INT_MAX ? LANTERN_E_SHAPE : LANTERN_OK;
+    return ((int64_t)plan->parts * cache->heads + 8) * plan->row_tiles > lantern::MOST_GROUPS ? LANTERN_E_SHAPE : LANTERN_OK;
 }
 
 }  // namespace
@@ -542,7 +542,7 @@ int lantern_attend_trees(const void* q, const int64_t* q_strides, const void* k,
     lantern::AttendPlan plan;
     int rc = attend_plan(dtype, B, M, q_heads, cache, table_width, &plan);
     if (rc != LANTERN_OK) return rc;
-    if (!(scale >= 0.f) || scale > FLT_MAX) return LANTERN_E_SHAPE;
+    if (!(scale >= 0.f) || scale > FLT_MAX / 2) return LANTERN_E_SHAPE;
     if (B == 0) return LANTERN_OK;
     rc = cache_memory(*cache);
     if (rc != LANTERN_OK) return rc;

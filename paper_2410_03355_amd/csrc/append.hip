@@ -453,6 +453,7 @@ static size_t lds_bytes(const lantern_cache& c) { return sizeof(T) * c.page_toke
 
 template <typename T, bool EIGHT, int EACH>
 static hipError_t launch_pages(const AppendArgs& a, hipStream_t stream) {
+    if ((int64_t)a.B * a.touched > MOST_GROUPS) return hipErrorInvalidConfiguration;
     const size_t lds = lds_bytes<T>(a.cache);
     const hipError_t e = allow_lds<append_pages_kernel<T, EIGHT, EACH>>(lds);
     if (e != hipSuccess) return e;
@@ -470,6 +471,7 @@ static hipError_t launch(const AppendArgs& a, hipStream_t stream) {
     // A wavefront holds 64 units: up to four times that in rows, and the accepted candidates of a tree, which are few
     if (a.path || a.T * units <= 4 * WAVE) {
         const int64_t items = 2 * (int64_t)a.B * a.touched * a.cache.heads;
+        if (items > MOST_GROUPS * NW) return hipErrorInvalidConfiguration;
         hipLaunchKernelGGL((append_rows_kernel<T, EIGHT>), dim3((unsigned)((items + NW - 1) / NW)), dim3(NT), 0, stream, a);
         return hipGetLastError();
     }

@@ -8,6 +8,8 @@
 
 namespace lantern {
 
+constexpr int64_t MOST_GROUPS = (1 << 24) - 1;      // workgroups of 256 along a grid's x: a launch has less than 2^32 threads there
+
 struct Strided {            // elements from one sequence, row and head to the next; a head's elements are dense
     int64_t seq, row, head;
 };

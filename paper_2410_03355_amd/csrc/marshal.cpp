@@ -14,6 +14,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <c10/core/GradMode.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -378,10 +379,10 @@ bool heads_type(const at::Tensor& t, lantern_dtype* type) {
     else return false;
     return true;
 }
-// [.., heads, D] with dense heads, `dims` of them, nothing empty.
+// [.., heads, D] with dense heads, `dims` of them, nothing empty, nothing that autograd records.
 const at::Tensor* heads_of(PyObject* o, int dims) {
     const at::Tensor* t = near(o);
-    if (!t || t->dim() != dims || t->stride(dims - 1) != 1) return nullptr;
+    if (!t || t->dim() != dims || t->stride(dims - 1) != 1 || (t->requires_grad() && c10::GradMode::is_enabled())) return nullptr;
     for (int i = 0; i < dims; ++i)
         if (t->size(i) < 1 || t->size(i) > INT_MAX) return nullptr;
     return t;
@@ -406,7 +407,7 @@ bool cache_of(PyObject* o, lantern_cache* c) {
 // positions [rows, axes], freqs, sections: a tuple of whole numbers
 bool rotation_of(PyObject* pos, PyObject* freqs, PyObject* sections, PyObject* inter, int64_t rows, lantern_rotation* r) {
     const at::Tensor *p = near(pos, at::kInt), *f = near(freqs, at::kFloat);
-    if (!p || !f || !PyTuple_CheckExact(sections) || !PyBool_Check(inter)) return false;
+    if (!p || !f || (f->requires_grad() && c10::GradMode::is_enabled()) || !PyTuple_CheckExact(sections) || !PyBool_Check(inter)) return false;
     const Py_ssize_t axes = PyTuple_GET_SIZE(sections);
     if (axes < 1 || axes > LANTERN_MAX_AXES || p->numel() != rows * axes) return false;
     *r = {p->const_data_ptr<int32_t>(), f->const_data_ptr<float>(), (int)axes, {0, 0, 0, 0}, inter == Py_True};

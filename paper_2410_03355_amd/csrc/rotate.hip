@@ -53,6 +53,7 @@ static hipError_t launch(RotateArgs a, hipStream_t stream) {
     const int per_block = NT / rotation_units<NP>(a.pairs, a.D);
     const int blocks = (int)(((int64_t)a.N + per_block - 1) / per_block), heads = a.q_heads + a.k_heads;
     // Few tokens: their heads are spread over blocks until there are some 8 wavefronts for each of the 256 CUs.
+    if (blocks > MOST_GROUPS) return hipErrorInvalidConfiguration;
     const int chunks = std::max(1, std::min(heads, 512 / std::max(1, blocks)));
     a.heads_per_block = (heads + chunks - 1) / chunks;
     hipLaunchKernelGGL((rotate_axes_kernel<T, NP, WIDE>), dim3(blocks, (heads + a.heads_per_block - 1) / a.heads_per_block), dim3(NT), 0,

@@ -80,7 +80,8 @@ def test_attend_refusals(lib):
         assert call(cache=_cache(**kw)) == getattr(B_, status), kw
     assert call(dtype=L.E4M3) == B_.E_DTYPE
     for kw in (dict(B=-1), dict(M=-1), dict(M=L.MAX_TREE + 1), dict(Hq=0), dict(Hq=-4), dict(Hq=6), dict(width=0), dict(width=2 ** 25),
-               dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=-1.0), dict(B=2 ** 28, M=255)):
+               dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=-1.0), dict(scale=3e38), dict(B=2 ** 28, M=255),
+               dict(B=2 ** 22)):      # 2^24 workgroups
         assert call(**kw) == B_.E_SHAPE, kw
     for kw in (dict(cache=None), dict(q=NUL), dict(qs=NUL), dict(k=NUL), dict(ks=NUL), dict(v=NUL), dict(vs=NUL), dict(table=NUL), dict(lengths=NUL),
                dict(out=NUL)):
@@ -142,9 +143,31 @@ def test_binding_refusals():
     assert c.v.shape == (4, 2, 32, 16) and c.k.dtype == torch.float8_e4m3fn and L.make_cache(4, 2, 16, 32, torch.bfloat16, "cpu").k_scale is None
 
 
+def test_gradients_that_are_not_formed():
+    """Recorded inputs are refused where there is no backward pass, before anything else is done with them."""
+    cache, table = ref.filled_cache(torch.Generator().manual_seed(0), [20], 2, 32, 16, True)
+    n = torch.tensor([20], dtype=torch.int32)
+    x, leaf = torch.zeros(1, 1, 2, 32), torch.zeros(1, 1, 2, 32, requires_grad=True)
+    pos, freqs = torch.zeros(1, 2, dtype=torch.int32), torch.ones(8)
+    for f in (lambda: L.attend_trees(leaf, x, x, None, cache, table, n), lambda: L.attend_trees(x, leaf, x, None, cache, table, n),
+              lambda: L.append_cache(cache, table, n, x, leaf)):
+        with pytest.raises(ValueError, match="no backward pass"):
+            f()
+    for kw in (dict(out=(leaf[0], None)), dict(freqs=freqs.clone().requires_grad_())):
+        with pytest.raises(ValueError, match="gradients are recorded"):
+            L.rotate_axes(leaf[0], None, pos, kw.pop("freqs", freqs), (4, 4), **kw)
+
+
+def test_a_workspace_with_gaps():
+    cache, table = ref.filled_cache(torch.Generator().manual_seed(0), [20], 2, 32, 16, True)
+    x = torch.zeros(1, 1, 2, 32)
+    with pytest.raises(ValueError, match="contiguous"):
+        L.attend_trees(x, x, x, None, cache, table, torch.tensor([20], dtype=torch.int32), workspace=torch.zeros(512, dtype=torch.uint8)[::2])
+
+
 def test_workspace_shrinks_with_enough_sequences(lib):
     """Sequences are split only while there are too few of them to fill the device."""
     cache = (torch.zeros(4, 20, 64, 64, dtype=torch.bfloat16), torch.zeros(4, 20, 64, 64, dtype=torch.bfloat16), None, None)
     assert L.attend_trees_workspace_bytes(torch.bfloat16, 64, 60, 20, cache, 12) == 0
     one = L.attend_trees_workspace_bytes(torch.bfloat16, 1, 0, 20, cache, 512)
-    assert one % (20 * 66 * 4) == 0 and one > 0
+    assert one % (20 * 66 * 4) == 8 and one > 8      # and where the sequence is cut

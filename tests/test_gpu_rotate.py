@@ -109,3 +109,32 @@ def test_streams_nothing_to_do_and_untouched_rest(lantern_gpu):
     assert bool(a[5, 1].isnan().all())
     a[5, 1] = want[5, 1]
     assert torch.equal(a, want)
+
+
+@pytest.mark.parametrize("inter", [True, False])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_autograd_turns_back(lantern_gpu, dtype, inter):
+    """Gradients of q, of a key head that several share, and of either alone; a gradient without dense heads; twice over."""
+    gen = torch.Generator().manual_seed(6)
+    N, D, sections = 21, 32, (5, 9)
+    pos = torch.randint(-50, 300, (N, 2), generator=gen, dtype=torch.int32).cuda()
+    args = (pos, torch.rand(14, generator=gen).cuda(), sections)
+    q = ref.normal(gen, N, 3, D).to(dtype).cuda().requires_grad_()
+    k = ref.normal(gen, N, 1, D).to(dtype).cuda().requires_grad_()
+    gq, gk = ref.normal(gen, N, 3, D).to(dtype).cuda(), ref.normal(gen, N, D, 4).to(dtype).cuda().transpose(1, 2)
+    tq, tk = lantern_gpu.rotate_axes(q, k.expand(N, 4, D), *args, interleaved=inter)
+    with torch.no_grad():
+        wq, wk = lantern_gpu.rotate_axes(q, k.expand(N, 4, D), *args, interleaved=inter)
+        bq, bk = lantern_gpu.rotate_axes(gq, gk.contiguous(), *args, interleaved=inter, inverse=True)
+    assert torch.equal(tq, wq) and torch.equal(tk, wk) and not wq.requires_grad
+    torch.autograd.backward([tq, tk], [gq, gk])
+    assert torch.equal(q.grad, bq)
+    half = torch.finfo(dtype).eps / 2      # torch's sum over the four heads: in fp32, then rounded once
+    room = half * bk.double().sum(1, keepdim=True).abs() + 4 * 2.0 ** -24 * bk.double().abs().sum(1, keepdim=True)
+    assert bool(((k.grad.double() - bk.double().sum(1, keepdim=True)).abs() <= room).all())
+    alone, none = lantern_gpu.rotate_axes(q, None, *args, interleaved=inter)
+    (again,) = torch.autograd.grad(alone, q, gq)
+    assert none is None and torch.equal(again, bq)
+    only_k = lantern_gpu.rotate_axes(q.detach(), k, *args, interleaved=inter)
+    (again,) = torch.autograd.grad(only_k[1], k, gk[:, :1].contiguous())
+    assert torch.equal(again, bk[:, :1]) and again.shape == k.shape
