@@ -907,20 +907,26 @@ __global__ __launch_bounds__(NT) void attend_join_kernel(AttendArgs a) {
 AttendPlan plan_attend(int dtype, int B, int M, int q_heads, const lantern_cache& c, int width) {
     AttendPlan p;
     const int64_t R = (int64_t)(M + 1) * (q_heads / c.heads);
+    const int64_t room = dtype == LANTERN_BF16 && c.D <= 64 ? 768 : 512;      // workgroups that fit the 256 CUs at once
+    const int64_t tokens = (int64_t)width * c.page_tokens, tile = c.dtype == LANTERN_E4M3 ? 64 : 32;
+    const int64_t useful = std::max<int64_t>(1, tokens / (tile * NW * 2));    // parts of two tiles to a wavefront at least
     // Tiles of 16 rows that a wavefront takes together: each conversion of a tile of tokens serves all of them.  Four (D <= 64, 246 registers)
-    // were no faster where they had all their use: 64 trees of 61 rows 55.1 us against 53.8 with two, one tree 14.8 against 11.3.
-    p.row_group = R <= 16 ? 1 : 2;
-    const int64_t room = dtype == LANTERN_BF16 && c.D <= 64 ? 768 : 512, tiles = (R + 16 * p.row_group - 1) / (16 * p.row_group);
+    // were no faster where they had all their use: 64 trees of 61 rows 55.1 us against 53.8 with two, one tree 14.8 against 11.3.  One, where
+    // all workgroups fit at once and sequences are not cut: a wavefront has less to do (one tree of 61 rows behind 640 tokens 9.9 us against 11.0, 8
+    // of 33 11.6 against 13.1, but 26 of 33 23.4 against 21.7, and long sequences behind 33 rows 32 against 27).  Also in fp32, bound by its
+    // products, where one leaves a sixth less of empty rows (20 trees of 33 rows 50 us against 61, of 66 97 against 102, but 132 rows 191
+    // against 192 and less with shorter heads).
+    const int64_t ones = (R + 15) / 16, twos = (R + 31) / 32;
+    const bool one = R <= 16 || (useful == 1 && B * c.heads * ones <= room) || (dtype == LANTERN_F32 && 6 * ones <= 10 * twos);
+    p.row_group = one ? 1 : 2;
+    const int64_t tiles = one ? ones : twos;
     // Where workgroups of one set of such tiles are more than fit at once, two wavefronts take two sets side by side: half the workgroups,
     // which bring own rows, tree and arguments for twice the work.  20 heads, trees of 61 rows: 64 sequences 45.5 us against 52.5, 39 30.5
     // against 32.9, 20 21.3 against 22.8, but one 15.4 against 11.1.  fp32 is bound by its products and loses (32 sequences 97 against 87).
-    p.abreast = dtype == LANTERN_BF16 && tiles > 1 && B * c.heads * tiles > room ? 2 : 1;
+    p.abreast = dtype == LANTERN_BF16 && !one && tiles > 1 && B * c.heads * tiles > room ? 2 : 1;
     p.row_tiles = (int)((tiles + p.abreast - 1) / p.abreast);
-    // Where sequences, heads and row tiles make fewer workgroups than fit the 256 CUs at once (two or three to a CU), sequences are cut:
-    // into parts of two tiles to a wavefront at least.
-    const int64_t groups = (int64_t)c.heads * p.row_tiles, tokens = (int64_t)width * c.page_tokens;
-    const int64_t tile = c.dtype == LANTERN_E4M3 ? 64 : 32;
-    const int64_t useful = std::max<int64_t>(1, tokens / (tile * NW * 2));
+    // Where sequences, heads and row tiles make fewer workgroups than fit, sequences are cut.
+    const int64_t groups = (int64_t)c.heads * p.row_tiles;
     const int64_t parts = std::min(room / groups, B * useful);
     p.parts = (int)(parts >= 2 * (int64_t)B ? parts : B);
     p.workspace = p.parts == B ? 0 : (size_t)p.parts * c.heads * R * (c.D + 2) * sizeof(float) + B * sizeof(int2);
