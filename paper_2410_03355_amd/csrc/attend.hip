@@ -17,7 +17,7 @@
 //
 // Measured (kernel time; 8-bit cache, bf16, unless said): 8 single tokens of 32 heads on 4 of 128 behind 4099 to 32768 tokens 32 us and 5 for the join,
 // 4.7 TB/s, where a large copy reaches 5.1; 64 trees of 61 rows, 20 heads of 64 over 120 to 690 tokens 45.5 us, bound by latency and issue (half of
-// the vector instructions are prologue, own rows and join); 4 trees of 33 rows, 32 heads on 8 of 128 behind 2000 to 16001 tokens 56 + 5 us, 317
+// the vector instructions are prologue, own rows and join); 4 trees of 33 rows, 32 heads on 8 of 128 behind 2000 to 16001 tokens 56 + 5 us, 319
 // TFLOP/s, bound by matrix and vector instructions that overlap by a fifth; one token over 577 tokens 9 us, five loads one after the other.
 #include <hip/hip_runtime.h>
 #include <float.h>

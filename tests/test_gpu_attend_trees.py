@@ -113,6 +113,18 @@ def test_more_sequences_than_fit_at_once(lantern_gpu, eight, B, G, Hk, M, D, pag
 
 @pytest.mark.parametrize("eight", [True, False])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("B,G,Hk,M,D", [(30, 1, 20, 24, 32), (12, 2, 22, 27, 64)])
+def test_two_tiles_of_rows_without_a_cut(lantern_gpu, eight, dtype, B, G, Hk, M, D):
+    """Many short sequences of 25 or 56 rows to a key head: each wavefront takes 32 of them."""
+    lengths = [(3, 70, 0, 129)[b % 4] for b in range(B)]
+    case = _case(D + B, B, M, G, Hk, D, 32, eight, dtype, lengths)
+    assert lantern_gpu.attend_trees_workspace_bytes(dtype, B, M, G * Hk, ref.on_gpu(case[4]), case[5].shape[1]) == 0
+    want, bound = ref.attend(*case)
+    _check(_gpu(lantern_gpu, *case), want, bound)
+
+
+@pytest.mark.parametrize("eight", [True, False])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_rows_that_are_not_there(lantern_gpu, eight, dtype):
     """Candidates with a parent out of range, and those behind them, have zero rows and are seen by nobody, whatever they hold."""
     case = list(_case(6, 3, 20, 2, 1, 64, 64, eight, dtype, (70, 0, -1)))
