@@ -12,6 +12,7 @@ takes that way: the same kernels and results, later launches.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import importlib.machinery
 import importlib.util
@@ -746,11 +747,19 @@ def _need_here(stream, *tensors):
         raise ValueError("all tensors and the stream must belong to the current device")
 
 
-def _made_for(stream, *tensors):
-    """Tensors allocated here for work on a stream of the caller's: their memory is not given away before that is done."""
+def _room(stream, size, dtype, device):
+    """Memory for work on `stream` (None: the current one), from that stream's own: what the current stream has freed may still be read or
+    written by work queued there, which another stream does not wait for."""
+    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+        return torch.empty(size, dtype=dtype, device=device)
+
+
+def _output(stream, size, dtype, device):
+    """The same for what the caller gets: once dropped it is given away when the current stream, which may read it, has come to that place."""
+    t = _room(stream, size, dtype, device)
     if stream is not None:
-        for t in tensors:
-            t.record_stream(stream)
+        t.record_stream(torch.cuda.current_stream())
+    return t
 
 
 def _strides(*values):
@@ -839,8 +848,7 @@ def rotate_axes(q, k, positions, freqs, sections, interleaved: bool = False, inv
     code = _dtype_code(q)
     rot = _rotation_args(positions, freqs, sections, interleaved, N)
     if out is None:
-        outs = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in ts]
-        _made_for(stream, *outs)
+        outs = [_output(stream, t.shape, t.dtype, t.device) for t in ts]
     else:
         outs = [t for t in out if t is not None]
         if len(outs) != len(ts) or any(o.shape != t.shape or o.dtype != t.dtype or (D > 1 and o.stride(2) != 1) for o, t in zip(outs, ts)):
@@ -890,8 +898,7 @@ def append_cache(cache, table, lengths, k, v, positions=None, freqs=None, sectio
     if path is not None and count is None:
         raise ValueError("path comes with count")
     _need_here(stream, *parts, table, lengths, k, v, positions, freqs, path, count)
-    out = torch.empty(B, dtype=torch.int32, device=k.device)
-    _made_for(stream, out)
+    out = _output(stream, B, torch.int32, k.device)
     rc = lib.lantern_append_cache(ctypes.byref(c), table.data_ptr(), table.shape[1], lengths.data_ptr(), B, T, k.data_ptr(),
                                   _strides(*k.stride()[:3]), v.data_ptr(), _strides(*v.stride()[:3]), _dtype_code(k),
                                   None if rot is None else ctypes.byref(rot), None if path is None else path.data_ptr(),
@@ -932,10 +939,8 @@ def attend_trees(q, k, v, parent, cache, table, lengths, scale=None, workspace=N
     code, Hq, width = _dtype_code(q), q.shape[2], table.shape[1]
     need = int(lib.lantern_attend_trees_workspace_bytes(code, B, T - 1, Hq, ctypes.byref(c), width))
     if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        _made_for(stream, workspace)
-    out = torch.empty((B, T, Hq, c.D), dtype=q.dtype, device=q.device)
-    _made_for(stream, out)
+        workspace = _room(stream, need, torch.uint8, q.device)
+    out = _output(stream, (B, T, Hq, c.D), q.dtype, q.device)
     rc = lib.lantern_attend_trees(q.data_ptr(), _strides(*q.stride()[:3]), k.data_ptr(), _strides(*k.stride()[:3]), v.data_ptr(),
                                   _strides(*v.stride()[:3]), code, B, T - 1, Hq, None if parent is None else parent.data_ptr(),
                                   ctypes.byref(c), table.data_ptr(), width, lengths.data_ptr(),

@@ -1,0 +1,84 @@
+"""What the Python half of the calls around a tree step does before and around the library's calls, seen on the host: the library is a stand-in
+that notes its calls, and tensors of host memory are let through."""
+import contextlib
+
+import pytest
+import torch
+
+import cache_reference as ref
+import paper_2410_03355_amd as L
+from paper_2410_03355_amd import binding
+
+
+class _Library:
+    def __init__(self):
+        self.called, self.workspace = [], 0
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.called.append((name, args))
+            return self.workspace if name.endswith("_bytes") else binding.OK
+        return call
+
+
+@pytest.fixture
+def lib(monkeypatch):
+    stand_in = _Library()
+    monkeypatch.setattr(binding, "load", lambda: stand_in)
+    monkeypatch.setattr(binding, "_marshal", binding._Declines())
+    monkeypatch.setattr(binding, "_need_here", lambda *a: None)
+    monkeypatch.setattr(binding, "_need_cuda", lambda *a: None)
+    monkeypatch.setattr(binding, "_stream_ptr", lambda stream: 0)
+    return stand_in
+
+
+def _calls(B=2, T=4, Hq=4, Hk=2, D=32):
+    """Arguments of each call that are right."""
+    gen = torch.Generator().manual_seed(0)
+    cache, table = ref.filled_cache(gen, [20 + 10 * b for b in range(B)], Hk, D, 16, True)
+    n = torch.tensor([20 + 10 * b for b in range(B)], dtype=torch.int32)
+    q, k, v = (torch.zeros(B, T, h, D) for h in (Hq, Hk, Hk))
+    pos, freqs = torch.zeros(B, T, 2, dtype=torch.int32), torch.ones(8)
+    return {
+        "rotate_axes": dict(q=q.flatten(0, 1), k=k.flatten(0, 1), positions=pos.flatten(0, 1), freqs=freqs, sections=(4, 4)),
+        "append_cache": dict(cache=cache, table=table, lengths=n, k=k, v=v, positions=pos, freqs=freqs, sections=(4, 4),
+                             path=torch.zeros(B, T - 1, dtype=torch.int32), count=torch.zeros(B, dtype=torch.int32)),
+        "attend_trees": dict(q=q, k=k, v=v, parent=torch.zeros(B * (T - 1), dtype=torch.int32), cache=cache, table=table, lengths=n),
+    }
+
+
+@pytest.mark.parametrize("name", ["rotate_axes", "append_cache", "attend_trees"])
+def test_memory_of_another_stream(lib, monkeypatch, name):
+    """With a stream of the caller's, outputs and workspace come from that stream's memory: what the current stream has freed may still be
+    read by work that is queued there and that the other stream does not wait for.  Outputs are not given away again before the
+    current stream, which reads them, has passed the place where they are dropped."""
+    kw, side, state = _calls()[name], object(), {"inside": 0}
+    made, kept = [], []
+
+    @contextlib.contextmanager
+    def on(stream):
+        assert stream is side
+        state["inside"] += 1
+        yield
+        state["inside"] -= 1
+
+    empty = torch.empty
+
+    def noted(*args, **kwargs):
+        t = empty(*args, **kwargs)
+        made.append((t.data_ptr(), state["inside"]))
+        return t
+
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: "current")
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: kept.append((t.data_ptr(), s)))
+    monkeypatch.setattr(torch, "empty", noted)
+    lib.workspace = 4096
+    got = getattr(L, name)(**kw, stream=side)
+    outs = got if isinstance(got, tuple) else (got,)
+    assert len(made) == len(outs) + (name == "attend_trees") and all(inside == 1 for _, inside in made)
+    assert all((o.data_ptr(), "current") in kept for o in outs)
+    made.clear()
+    kept.clear()
+    getattr(L, name)(**kw)
+    assert all(inside == 0 for _, inside in made) and not kept
