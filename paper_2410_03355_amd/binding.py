@@ -205,6 +205,21 @@ def _stream_ptr(stream) -> int:
     return int(s.cuda_stream)
 
 
+def _room(stream, size, dtype, device):
+    """Memory for work on `stream` (None: the current one), from that stream's own: what the current stream has freed may still be read or
+    written by work queued there, which another stream does not wait for."""
+    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+        return torch.empty(size, dtype=dtype, device=device)
+
+
+def _output(stream, size, dtype, device):
+    """The same for what the caller gets: once dropped it is given away when the current stream, which may read it, has come to that place."""
+    t = _room(stream, size, dtype, device)
+    if stream is not None:
+        t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
 def _need_cuda(*tensors):
     for t in tensors:
         if t is not None and not t.is_cuda:
@@ -231,14 +246,14 @@ def build_knn(codebook: torch.Tensor, k: int, metric: str = "l2", stream=None, r
     if nbytes == 0:
         raise LanternError(E_SHAPE, "lantern_build_knn_workspace_bytes")
     if workspace is None:
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=codebook.device)
+        ws = (_output if return_stats else _room)(stream, nbytes, torch.uint8, codebook.device)
     else:
         _need_cuda(workspace)
         if workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.numel() < nbytes:
             raise ValueError("workspace must be a contiguous uint8 tensor of at least knn_workspace_bytes")
         ws = workspace
     if out is None:
-        out = torch.empty((V, k), dtype=torch.int32, device=codebook.device)
+        out = _output(stream, (V, k), torch.int32, codebook.device)
     else:
         _need_cuda(out)
         if out.dtype != torch.int32 or tuple(out.shape) != (V, k) or not out.is_contiguous():
@@ -248,8 +263,6 @@ def build_knn(codebook: torch.Tensor, k: int, metric: str = "l2", stream=None, r
                                       out.data_ptr(), ws.data_ptr(), ws.numel(), _stream_ptr(stream))
     if rc != OK:
         raise LanternError(rc, "lantern_build_knn")
-    if workspace is None:
-        ws.record_stream(torch.cuda.current_stream() if stream is None else stream)
     if return_stats:
         return out, ws[:4].view(torch.int32)[0]
     return out
@@ -321,8 +334,8 @@ def verify(target_logits, draft_logits, draft_tokens, knn, delta: float, uniform
             return got
     N, V, k = _check_verify_args(target_logits, draft_logits, draft_tokens, knn, uniforms)
     dev = target_logits.device
-    acc = torch.empty(N, dtype=torch.int32, device=dev) if out_accept is None else out_accept
-    res = torch.empty(N, dtype=torch.int32, device=dev) if out_resample is None else out_resample
+    acc = _output(stream, N, torch.int32, dev) if out_accept is None else out_accept
+    res = _output(stream, N, torch.int32, dev) if out_resample is None else out_resample
     rc = lib.lantern_verify(target_logits.data_ptr(), draft_logits.data_ptr(),
                             _dtype_code(target_logits), N, V, target_logits.stride(0) if N > 1 else V,
                             draft_tokens.data_ptr(), knn.data_ptr(), k, float(delta),
@@ -345,13 +358,13 @@ def verify_ex(target_logits, draft_logits, draft_tokens, knn, delta: float, unif
     N, V, k = _check_verify_args(target_logits, draft_logits, draft_tokens, knn, uniforms)
     dev = target_logits.device
     out = {
-        "accept": torch.empty(N, dtype=torch.int32, device=dev),
-        "resample": torch.empty(N, dtype=torch.int32, device=dev),
-        "accept_prob": torch.empty(N, dtype=torch.float32, device=dev),
-        "mass": torch.empty(N, dtype=torch.float32, device=dev),
-        "g_tok": torch.empty(N, dtype=torch.float32, device=dev),
-        "a_size": torch.empty(N, dtype=torch.int32, device=dev),
-        "path": torch.empty(N, dtype=torch.int32, device=dev),
+        "accept": _output(stream, N, torch.int32, dev),
+        "resample": _output(stream, N, torch.int32, dev),
+        "accept_prob": _output(stream, N, torch.float32, dev),
+        "mass": _output(stream, N, torch.float32, dev),
+        "g_tok": _output(stream, N, torch.float32, dev),
+        "a_size": _output(stream, N, torch.int32, dev),
+        "path": _output(stream, N, torch.int32, dev),
     }
     common_in = (target_logits.data_ptr(), draft_logits.data_ptr(), _dtype_code(target_logits), N, V,
                  target_logits.stride(0) if N > 1 else V, draft_tokens.data_ptr(), knn.data_ptr(), k)
@@ -386,9 +399,9 @@ def verify_greedy(target_logits, draft_tokens, knn, delta: float, stream=None, w
     if not (draft_tokens.is_contiguous() and knn.is_contiguous()):
         raise ValueError("draft_tokens and knn must be contiguous")
     dev = target_logits.device
-    acc = torch.empty(N, dtype=torch.int32, device=dev)
-    tok = torch.empty(N, dtype=torch.int32, device=dev)
-    path = torch.empty(N, dtype=torch.int32, device=dev) if want_path else None
+    acc = _output(stream, N, torch.int32, dev)
+    tok = _output(stream, N, torch.int32, dev)
+    path = _output(stream, N, torch.int32, dev) if want_path else None
     rc = lib.lantern_verify_greedy(target_logits.data_ptr(), _dtype_code(target_logits), N, V,
                                    target_logits.stride(0) if N > 1 else V, draft_tokens.data_ptr(),
                                    knn.data_ptr(), int(knn.shape[1]), float(delta), acc.data_ptr(),
@@ -415,8 +428,8 @@ def accept_chains(accept, resample, L: int, stream=None):
     if not (accept.is_contiguous() and resample.is_contiguous()):
         raise ValueError("accept and resample must be contiguous")
     B = accept.numel() // L
-    kept = torch.empty(B, dtype=torch.int32, device=accept.device)
-    nxt = torch.empty(B, dtype=torch.int32, device=accept.device)
+    kept = _output(stream, B, torch.int32, accept.device)
+    nxt = _output(stream, B, torch.int32, accept.device)
     rc = lib.lantern_accept_chains(accept.data_ptr(), resample.data_ptr(), B, int(L), kept.data_ptr(),
                                    nxt.data_ptr(), _stream_ptr(stream))
     if rc != OK:
@@ -455,8 +468,8 @@ def verify_rows(target_logits, draft_logits, row_index, draft_tokens, knn, delta
     if not (draft_tokens.is_contiguous() and knn.is_contiguous() and uniforms.is_contiguous()):
         raise ValueError("draft_tokens, knn and uniforms must be contiguous")
     dev = target_logits.device
-    acc = torch.empty(N, dtype=torch.int32, device=dev)
-    res = torch.empty(N, dtype=torch.int32, device=dev)
+    acc = _output(stream, N, torch.int32, dev)
+    res = _output(stream, N, torch.int32, dev)
     rc = lib.lantern_verify_rows(target_logits.data_ptr(), draft_logits.data_ptr(), _dtype_code(target_logits),
                                  R, V, target_logits.stride(0) if R > 1 else V, row_index.data_ptr(), N,
                                  draft_tokens.data_ptr(), knn.data_ptr(), int(knn.shape[1]),
@@ -485,8 +498,8 @@ def verify_greedy_rows(target_logits, row_index, draft_tokens, knn, delta: float
     if knn.dim() != 2 or knn.shape[0] != V or not (draft_tokens.is_contiguous() and knn.is_contiguous()):
         raise ValueError("the table must be a contiguous [V, k] tensor, the tokens contiguous")
     dev = target_logits.device
-    acc = torch.empty(N, dtype=torch.int32, device=dev)
-    tok = torch.empty(N, dtype=torch.int32, device=dev)
+    acc = _output(stream, N, torch.int32, dev)
+    tok = _output(stream, N, torch.int32, dev)
     rc = lib.lantern_verify_greedy_rows(target_logits.data_ptr(), _dtype_code(target_logits), R, V,
                                         target_logits.stride(0) if R > 1 else V, row_index.data_ptr(), N,
                                         draft_tokens.data_ptr(), knn.data_ptr(), int(knn.shape[1]), float(delta),
@@ -513,9 +526,9 @@ def accept_trees(accept, resample, parent, M: int, stream=None):
         raise ValueError("accept, resample and parent must hold B*M rows")
     B = accept.numel() // M
     dev = accept.device
-    n = torch.empty(B, dtype=torch.int32, device=dev)
-    path = torch.empty((B, M), dtype=torch.int32, device=dev)
-    nxt = torch.empty(B, dtype=torch.int32, device=dev)
+    n = _output(stream, B, torch.int32, dev)
+    path = _output(stream, (B, M), torch.int32, dev)
+    nxt = _output(stream, B, torch.int32, dev)
     rc = lib.lantern_accept_trees(accept.data_ptr(), None if resample is None else resample.data_ptr(),
                                   parent.data_ptr(), B, int(M),
                                   n.data_ptr(), path.data_ptr(), nxt.data_ptr(), _stream_ptr(stream))
@@ -530,7 +543,7 @@ RANDOM_MAX_K = 4096
 def build_random(V: int, k: int, seed: int, device="cuda", stream=None):
     """lantern_build_random; returns the [V, k] int32 table on the device."""
     lib = load()
-    out = torch.empty((V, k), dtype=torch.int32, device=device)
+    out = _output(stream, (V, k), torch.int32, device)
     rc = lib.lantern_build_random(int(V), int(k), int(seed) & 0xFFFFFFFFFFFFFFFF, out.data_ptr(),
                                   _stream_ptr(stream))
     if rc != OK:
@@ -571,8 +584,8 @@ def decide_rows(target_logits, draft_logits, row_index, draft_tokens, knn, delta
         if got is not None:
             return _checked_status(got, "lantern_decide_rows")
     R, V, N, stride = _rows_args(target_logits, draft_logits, row_index, draft_tokens, knn, uniforms)
-    acc = torch.empty(N, dtype=torch.int32, device=target_logits.device)
-    path = torch.empty(N, dtype=torch.int32, device=target_logits.device) if want_path else None
+    acc = _output(stream, N, torch.int32, target_logits.device)
+    path = _output(stream, N, torch.int32, target_logits.device) if want_path else None
     rc = lib.lantern_decide_rows(target_logits.data_ptr(), draft_logits.data_ptr(), _dtype_code(target_logits),
                                  R, V, stride, None if row_index is None else row_index.data_ptr(), N,
                                  draft_tokens.data_ptr(), knn.data_ptr(), int(knn.shape[1]),
@@ -592,7 +605,7 @@ def resample_selected(target_logits, draft_logits, row_index, draft_tokens, knn,
     _need_cuda(select)
     if select.dtype != torch.int32 or not select.is_contiguous():
         raise TypeError("select must be a contiguous int32 tensor")
-    out = torch.empty(select.numel(), dtype=torch.int32, device=target_logits.device)
+    out = _output(stream, select.numel(), torch.int32, target_logits.device)
     rc = lib.lantern_resample_selected(target_logits.data_ptr(), draft_logits.data_ptr(),
                                        _dtype_code(target_logits), R, V, stride,
                                        None if row_index is None else row_index.data_ptr(), N,
@@ -619,10 +632,10 @@ def verify_trees(target_logits, draft_logits, row_index, parent, M: int, draft_t
         raise ValueError("parent must be a contiguous int32 tensor of B*M entries")
     B = N // M
     dev = target_logits.device
-    acc = torch.empty(N, dtype=torch.int32, device=dev)
-    n = torch.empty(B, dtype=torch.int32, device=dev)
-    path = torch.empty((B, M), dtype=torch.int32, device=dev)
-    nxt = torch.empty(B, dtype=torch.int32, device=dev)
+    acc = _output(stream, N, torch.int32, dev)
+    n = _output(stream, B, torch.int32, dev)
+    path = _output(stream, (B, M), torch.int32, dev)
+    nxt = _output(stream, B, torch.int32, dev)
     rc = lib.lantern_verify_trees(target_logits.data_ptr(), draft_logits.data_ptr(), _dtype_code(target_logits),
                                   R, V, stride, None if row_index is None else row_index.data_ptr(),
                                   parent.data_ptr(), B, int(M),
@@ -653,11 +666,11 @@ def verify_trees_sequential(target_logits, draft_logits, row_index, parent, M: i
     dev = target_logits.device
     need = int(lib.lantern_verify_trees_sequential_workspace_bytes(B, int(M), V))
     if workspace is None:
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        workspace = _room(stream, max(need, 256), torch.uint8, dev)
     _need_cuda(workspace)
-    n = torch.empty(B, dtype=torch.int32, device=dev)
-    path = torch.empty((B, M), dtype=torch.int32, device=dev)
-    nxt = torch.empty(B, dtype=torch.int32, device=dev)
+    n = _output(stream, B, torch.int32, dev)
+    path = _output(stream, (B, M), torch.int32, dev)
+    nxt = _output(stream, B, torch.int32, dev)
     rc = lib.lantern_verify_trees_sequential(target_logits.data_ptr(), draft_logits.data_ptr(),
                                              _dtype_code(target_logits), R, V, stride,
                                              None if row_index is None else row_index.data_ptr(),
@@ -700,11 +713,11 @@ def verify_trees_greedy(target_logits, row_index, parent, M: int, draft_tokens, 
         raise ValueError("shape mismatch between parent, tokens and the table")
     B = N // M
     dev = target_logits.device
-    acc = torch.empty(N, dtype=torch.int32, device=dev)
-    tok = torch.empty(N, dtype=torch.int32, device=dev)
-    n = torch.empty(B, dtype=torch.int32, device=dev)
-    path = torch.empty((B, M), dtype=torch.int32, device=dev)
-    nxt = torch.empty(B, dtype=torch.int32, device=dev)
+    acc = _output(stream, N, torch.int32, dev)
+    tok = _output(stream, N, torch.int32, dev)
+    n = _output(stream, B, torch.int32, dev)
+    path = _output(stream, (B, M), torch.int32, dev)
+    nxt = _output(stream, B, torch.int32, dev)
     rc = lib.lantern_verify_trees_greedy(target_logits.data_ptr(), _dtype_code(target_logits), R, V,
                                          target_logits.stride(0) if R > 1 else V,
                                          None if row_index is None else row_index.data_ptr(), parent.data_ptr(), B,
@@ -745,21 +758,6 @@ def _need_here(stream, *tensors):
     here = torch.cuda.current_device()
     if any(t is not None and t.device.index != here for t in tensors) or (stream is not None and stream.device.index != here):
         raise ValueError("all tensors and the stream must belong to the current device")
-
-
-def _room(stream, size, dtype, device):
-    """Memory for work on `stream` (None: the current one), from that stream's own: what the current stream has freed may still be read or
-    written by work queued there, which another stream does not wait for."""
-    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-        return torch.empty(size, dtype=dtype, device=device)
-
-
-def _output(stream, size, dtype, device):
-    """The same for what the caller gets: once dropped it is given away when the current stream, which may read it, has come to that place."""
-    t = _room(stream, size, dtype, device)
-    if stream is not None:
-        t.record_stream(torch.cuda.current_stream())
-    return t
 
 
 def _strides(*values):
