@@ -76,9 +76,10 @@ struct Where {
             if (reports) a.out_lengths[b] = start;
             return;
         }
-        const int told = a.count ? a.count[b] : a.T - (a.path ? 1 : 0);
-        n = a.path ? told + 1 : told;
-        bool bad = told < 0 || n > a.T || (int64_t)start + n > (int64_t)a.width << a.page_shift;
+        const int most = a.T - (a.path ? 1 : 0), told = a.count ? a.count[b] : most;
+        bool bad = told < 0 || told > most;      // a count may be anything: looked at before it is added to
+        n = bad ? 0 : told + a.T - most;
+        bad |= (int64_t)start + n > (int64_t)a.width << a.page_shift;
         if (!bad && n > 0) {
             const int first_page = start >> a.page_shift, pages = ((start + n - 1) >> a.page_shift) - first_page + 1;
             for (int i = lane; i < pages; i += WAVE) {

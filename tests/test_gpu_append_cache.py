@@ -178,3 +178,24 @@ def test_strides_streams_and_far_pages(lantern_gpu):
         side.synchronize()
         assert got.tolist() == [140]
         _same([t[at] for t in big], [t[:2] for t in want])
+
+
+@pytest.mark.parametrize("T", [6, 200])
+@pytest.mark.parametrize("way", ["path", "rows"])
+def test_counts_of_any_value(lantern_gpu, way, T):
+    """Counts up to the ends of their type are refused like any that is beyond the rows; the largest that is right is served."""
+    gen = torch.Generator().manual_seed(T)
+    Hk, D, page = 2, 32, 16
+    most = T - 1 if way == "path" else T
+    counts = (2 ** 31 - 1, 2 ** 31 - 2, -2 ** 31, most + 1, most, 2 ** 31 - 1 - 12, 0)
+    B = len(counts)
+    cache, table = ref.filled_cache(gen, [12 + T] * B, Hk, D, page, True, rubbish=False)
+    path = torch.arange(T - 1, dtype=torch.int32).repeat(B, 1) if way == "path" else None
+    lengths, count = torch.full((B,), 12, dtype=torch.int32), torch.tensor(counts, dtype=torch.int32)
+    k, v = _rows(gen, B, T, Hk, D, torch.bfloat16)
+    dev = ref.on_gpu(cache)
+    got = lantern_gpu.append_cache(dev, table.cuda(), lengths.cuda(), k.cuda(), v.cuda(), path=None if path is None else path.cuda(), count=count.cuda())
+    kept = [4, 6]
+    want, ends = ref.append(cache, table[kept], [12, 12], k[kept], v[kept], None if path is None else path[kept], count[kept])
+    assert got.tolist() == [-2, -2, -2, -2, int(ends[0]), -2, int(ends[1])]
+    _same(dev, want)
