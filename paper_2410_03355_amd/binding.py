@@ -807,6 +807,18 @@ def _wants_gradients(*tensors) -> bool:
     return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
 
 
+def _no_tangents(*tensors):
+    if any(t is not None and torch.autograd.forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise ValueError("forward-mode derivatives are not formed here: a tangent would be lost")
+
+
+def _nothing_recorded(*tensors):
+    """Where there is no derivative of either mode: none of these may ask for one."""
+    _no_tangents(*tensors)
+    if _wants_gradients(*tensors):
+        raise ValueError("there is no backward pass here: call it under torch.no_grad()")
+
+
 class _Turned(torch.autograd.Function):
     """rotate_axes where gradients are wanted: turning is orthogonal, so theirs is to turn back."""
 
@@ -827,7 +839,8 @@ def rotate_axes(q, k, positions, freqs, sections, interleaved: bool = False, inv
     """lantern_rotate_axes: q [N, heads, D] and k [N, heads, D] (or None) turned by positions [N, axes]; sections: pairs of
     each axis, freqs [their sum].  Returns (q, k) turned, new tensors or those of `out` (a pair, which may be q and k
     themselves).  inverse turns back, which is the gradient: it takes the outputs' gradients to the inputs'.  Where autograd
-    records q or k that is done in their backward pass (with out or stream such a call is refused; freqs have no gradient)."""
+    records q or k that is done in their backward pass (with out or stream such a call is refused; freqs have no gradient, and there are no
+    forward-mode derivatives: tangents are refused)."""
     lib = load()
     if out is None and stream is None:
         got = _marshal.rotate_axes(q, k, positions, freqs, sections, interleaved, inverse)
@@ -837,6 +850,7 @@ def rotate_axes(q, k, positions, freqs, sections, interleaved: bool = False, inv
     for t in ts:
         if t.dim() != 3 or t.shape[0] != q.shape[0] or t.shape[2] != q.shape[2] or t.dtype != q.dtype or (t.shape[2] > 1 and t.stride(2) != 1):
             raise ValueError("q and k must be [N, heads, D] of the same N, D and dtype, with dense heads")
+    _no_tangents(*ts, freqs)
     if _wants_gradients(*ts, freqs):
         if out is not None or stream is not None or freqs.requires_grad:
             raise ValueError("gradients are recorded without out and stream, and freqs have none")
@@ -879,8 +893,7 @@ def append_cache(cache, table, lengths, k, v, positions=None, freqs=None, sectio
         got = _marshal.append_cache(cache, table, lengths, k, v, positions, freqs, sections, interleaved, path, count)
         if got is not None:
             return _checked_status(got, "lantern_append_cache")
-    if _wants_gradients(k, v):
-        raise ValueError("there is no backward pass here: call it under torch.no_grad()")
+    _nothing_recorded(k, v, freqs, *cache)
     c, parts = _cache_args(cache)
     _rows_of_cache(c, k, v)
     B, T = k.shape[:2]
@@ -921,8 +934,7 @@ def attend_trees(q, k, v, parent, cache, table, lengths, scale=None, workspace=N
         got = _marshal.attend_trees(q, k, v, parent, cache, table, lengths, scale, workspace)
         if got is not None:
             return _checked_status(got, "lantern_attend_trees")
-    if _wants_gradients(q, k, v):
-        raise ValueError("there is no backward pass here: call it under torch.no_grad()")
+    _nothing_recorded(q, k, v, *cache)
     c, parts = _cache_args(cache)
     _rows_of_cache(c, k, v)
     B, T = k.shape[:2]

@@ -379,10 +379,12 @@ bool heads_type(const at::Tensor& t, lantern_dtype* type) {
     else return false;
     return true;
 }
+// What autograd records, backwards or forwards: these calls are Python's.
+bool recorded(const at::Tensor& t) { return (t.requires_grad() && c10::GradMode::is_enabled()) || t._fw_grad(0).defined(); }
 // [.., heads, D] with dense heads, `dims` of them, nothing empty, nothing that autograd records.
 const at::Tensor* heads_of(PyObject* o, int dims) {
     const at::Tensor* t = near(o);
-    if (!t || t->dim() != dims || t->stride(dims - 1) != 1 || (t->requires_grad() && c10::GradMode::is_enabled())) return nullptr;
+    if (!t || t->dim() != dims || t->stride(dims - 1) != 1 || recorded(*t)) return nullptr;
     for (int i = 0; i < dims; ++i)
         if (t->size(i) < 1 || t->size(i) > INT_MAX) return nullptr;
     return t;
@@ -393,12 +395,14 @@ bool cache_of(PyObject* o, lantern_cache* c) {
     if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) return false;
     const at::Tensor *k = near(PyTuple_GET_ITEM(o, 0)), *v = near(PyTuple_GET_ITEM(o, 1));
     if (!k || !v || k->dim() != 4 || v->dim() != 4 || !k->is_contiguous() || !v->is_contiguous() || k->scalar_type() != v->scalar_type() ||
-        v->size(0) != k->size(0) || v->size(1) != k->size(1) || v->size(2) != k->size(3) || v->size(3) != k->size(2) || k->size(0) > INT_MAX)
+        v->size(0) != k->size(0) || v->size(1) != k->size(1) || v->size(2) != k->size(3) || v->size(3) != k->size(2) || k->size(0) > INT_MAX || recorded(*k) || recorded(*v))
         return false;
     *c = {k->data_ptr(), v->data_ptr(), nullptr, nullptr, LANTERN_BF16, (int)k->size(0), (int)k->size(1), (int)k->size(2), (int)k->size(3)};
     if (k->scalar_type() == at::kBFloat16) return true;
     const at::Tensor *ks = near(PyTuple_GET_ITEM(o, 2), at::kFloat), *vs = near(PyTuple_GET_ITEM(o, 3), at::kFloat);
-    if (k->scalar_type() != at::kFloat8_e4m3fn || !ks || !vs || ks->sizes() != k->sizes().slice(0, 2) || vs->sizes() != ks->sizes()) return false;
+    if (k->scalar_type() != at::kFloat8_e4m3fn || !ks || !vs || ks->sizes() != k->sizes().slice(0, 2) || vs->sizes() != ks->sizes() || recorded(*ks) ||
+        recorded(*vs))
+        return false;
     c->k_scale = ks->data_ptr<float>();
     c->v_scale = vs->data_ptr<float>();
     c->dtype = LANTERN_E4M3;
@@ -407,7 +411,7 @@ bool cache_of(PyObject* o, lantern_cache* c) {
 // positions [rows, axes], freqs, sections: a tuple of whole numbers
 bool rotation_of(PyObject* pos, PyObject* freqs, PyObject* sections, PyObject* inter, int64_t rows, lantern_rotation* r) {
     const at::Tensor *p = near(pos, at::kInt), *f = near(freqs, at::kFloat);
-    if (!p || !f || (f->requires_grad() && c10::GradMode::is_enabled()) || !PyTuple_CheckExact(sections) || !PyBool_Check(inter)) return false;
+    if (!p || !f || recorded(*f) || !PyTuple_CheckExact(sections) || !PyBool_Check(inter)) return false;
     const Py_ssize_t axes = PyTuple_GET_SIZE(sections);
     if (axes < 1 || axes > LANTERN_MAX_AXES || p->numel() != rows * axes) return false;
     *r = {p->const_data_ptr<int32_t>(), f->const_data_ptr<float>(), (int)axes, {0, 0, 0, 0}, inter == Py_True};

@@ -82,3 +82,44 @@ def test_memory_of_another_stream(lib, monkeypatch, name):
     kept.clear()
     getattr(L, name)(**kw)
     assert all(inside == 0 for _, inside in made) and not kept
+
+
+FLOATS = {"rotate_axes": ("q", "k", "freqs"), "append_cache": ("k", "v", "freqs"), "attend_trees": ("q", "k", "v")}
+
+
+@pytest.mark.parametrize("name,which", [(n, w) for n, ws in FLOATS.items() for w in ws])
+def test_tangents_are_refused(lib, name, which):
+    """A dual tensor would come back without its tangent."""
+    kw = _calls()[name]
+    with torch.autograd.forward_ad.dual_level():
+        plain, kw[which] = kw[which], torch.autograd.forward_ad.make_dual(kw[which], torch.ones_like(kw[which]))
+        with pytest.raises(ValueError, match="forward-mode"):
+            getattr(L, name)(**kw)
+        getattr(L, name)(**{**kw, which: plain})
+        with torch.autograd.forward_ad._set_fwd_grad_enabled(False):
+            getattr(L, name)(**kw)
+
+
+@pytest.mark.parametrize("name", ["append_cache", "attend_trees"])
+@pytest.mark.parametrize("i,eight", [(0, False), (1, False), (2, True), (3, True)])
+def test_a_cache_that_wants_gradients(lib, name, i, eight):
+    """Keys, values and scales of a cache have none either: refused where they are recorded, served where nothing is."""
+    kw = _calls()[name]
+    cache = list(kw["cache"]) if eight else list(L.make_cache(9, 2, 16, 32, torch.bfloat16, "cpu"))
+    cache[i] = cache[i].detach().clone().requires_grad_()
+    kw["cache"] = tuple(cache)
+    with pytest.raises(ValueError, match="no backward pass"):
+        getattr(L, name)(**kw)
+    assert not any(n == "lantern_" + name for n, _ in lib.called)
+    with torch.no_grad():
+        getattr(L, name)(**kw)
+    assert any(n == "lantern_" + name for n, _ in lib.called)
+
+
+def test_freqs_that_want_gradients(lib):
+    kw = _calls()["append_cache"]
+    kw["freqs"] = kw["freqs"].clone().requires_grad_()
+    with pytest.raises(ValueError, match="no backward pass"):
+        L.append_cache(**kw)
+    with torch.no_grad():
+        L.append_cache(**kw)
