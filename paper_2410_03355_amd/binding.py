@@ -906,8 +906,8 @@ def append_cache(cache, table, lengths, k, v, positions=None, freqs=None, sectio
     for t, n in ((path, B * (T - 1)), (count, B)):
         if t is not None and (t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous()):
             raise ValueError("path must be a contiguous int32 [B, T-1], count a contiguous int32 [B]")
-    if path is not None and count is None:
-        raise ValueError("path comes with count")
+    if path is not None and (count is None or T < 2):
+        raise ValueError("path comes with count, and with rows for its candidates")
     _need_here(stream, *parts, table, lengths, k, v, positions, freqs, path, count)
     out = _output(stream, B, torch.int32, k.device)
     rc = lib.lantern_append_cache(ctypes.byref(c), table.data_ptr(), table.shape[1], lengths.data_ptr(), B, T, k.data_ptr(),

@@ -461,7 +461,7 @@ PyObject* append_cache(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     ORDINARY(11, cache_of(a[0], &c) && (k = heads_of(a[3], 4)) && (v = heads_of(a[4], 4)) && alike(*k, *v) && heads_type(*k, &type) &&
                      k->size(2) == c.heads && k->size(3) == c.D && table_of(a[1], a[2], k->size(0), &table, &lengths) &&
                      (a[5] == Py_None || rotation_of(a[5], a[6], a[7], a[8], rows(), &r)) &&
-                     (a[9] == Py_None || ((path = near(a[9], at::kInt)) && path->numel() == rows() - k->size(0) && a[10] != Py_None)) &&
+                     (a[9] == Py_None || (k->size(1) > 1 && (path = near(a[9], at::kInt)) && path->numel() == rows() - k->size(0) && a[10] != Py_None)) &&
                      (a[10] == Py_None || ((some = near(a[10], at::kInt)) && some->numel() == k->size(0))))
     at::Tensor out;
     int status = 0;

@@ -123,3 +123,13 @@ def test_freqs_that_want_gradients(lib):
         L.append_cache(**kw)
     with torch.no_grad():
         L.append_cache(**kw)
+
+
+def test_a_path_without_candidates(lib):
+    """An empty path has no address, which the library takes for none: the first count rows, none of them, in the place of row 0."""
+    kw = _calls(T=1)["append_cache"]
+    assert kw["path"].numel() == 0 and kw["path"].data_ptr() == 0
+    with pytest.raises(ValueError, match="rows for its candidates"):
+        L.append_cache(**kw)
+    assert not lib.called
+    L.append_cache(**{**kw, "path": None})

@@ -86,3 +86,16 @@ def test_declined(lantern_gpu):
     a, b = lantern_gpu.rotate_axes(*calls["rotate_axes"][:4], [12, 8], True)       # a list of sections goes the general way
     c, d = lantern_gpu.rotate_axes(*calls["rotate_axes"])
     assert torch.equal(a, c) and torch.equal(b, d)
+
+
+def test_a_path_without_candidates(lantern_gpu):
+    """An empty path has no address: declined, and refused by Python."""
+    cache, calls = _calls(True, torch.bfloat16)
+    args = list(calls["append_cache"])
+    args[3:6] = [x[:, :1].contiguous() for x in args[3:6]]
+    args[9] = args[9][:, :0].contiguous()
+    before = cache[0].view(torch.uint8).clone()
+    assert binding._marshal.append_cache(*args) is None
+    with pytest.raises(ValueError, match="rows for its candidates"):
+        lantern_gpu.append_cache(*args)
+    assert torch.equal(cache[0].view(torch.uint8), before)
