@@ -760,6 +760,12 @@ def _need_here(stream, *tensors):
         raise ValueError("all tensors and the stream must belong to the current device")
 
 
+def _fits(*sizes):
+    """Sizes that the library takes as 32-bit integers: ctypes would cut them off."""
+    if any(ctypes.c_int(n).value != n for n in sizes):
+        raise ValueError("sizes must fit 32 bits")
+
+
 def _strides(*values):
     return (ctypes.c_int64 * len(values))(*values)
 
@@ -770,6 +776,7 @@ def _cache_args(cache):
     if k.dim() != 4 or v.dim() != 4 or not (k.is_contiguous() and v.is_contiguous()):
         raise ValueError("the cache must be two contiguous tensors, [pages, heads, page_tokens, D] and [pages, heads, D, page_tokens]")
     pages, heads, page_tokens, D = k.shape
+    _fits(*k.shape)
     if tuple(v.shape) != (pages, heads, D, page_tokens) or k.dtype != v.dtype:
         raise ValueError("the cache's keys and values must have the same sizes and dtype")
     scales = ()
@@ -791,10 +798,12 @@ def _table_args(table, lengths, B):
     if table.dim() != 2 or table.shape[0] != B or table.shape[1] < 1 or lengths.numel() != B or \
             not (table.is_contiguous() and lengths.is_contiguous()):
         raise ValueError("table must be contiguous [B, pages of a sequence], lengths contiguous [B]")
+    _fits(*table.shape)
 
 
 def _rotation_args(positions, freqs, sections, interleaved, rows: int):
     sections = tuple(int(n) for n in sections)
+    _fits(*sections)
     if positions.dtype != torch.int32 or freqs.dtype != torch.float32:
         raise TypeError("positions must be int32, freqs float32")
     if not 1 <= len(sections) <= MAX_AXES or positions.numel() != rows * len(sections) or freqs.numel() != sum(sections) or \
@@ -850,6 +859,7 @@ def rotate_axes(q, k, positions, freqs, sections, interleaved: bool = False, inv
     for t in ts:
         if t.dim() != 3 or t.shape[0] != q.shape[0] or t.shape[2] != q.shape[2] or t.dtype != q.dtype or (t.shape[2] > 1 and t.stride(2) != 1):
             raise ValueError("q and k must be [N, heads, D] of the same N, D and dtype, with dense heads")
+        _fits(*t.shape)
     _no_tangents(*ts, freqs)
     if _wants_gradients(*ts, freqs):
         if out is not None or stream is not None or freqs.requires_grad:
@@ -881,6 +891,7 @@ def _rows_of_cache(cache: _Cache, k, v):
     if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.shape[2] != cache.heads or k.shape[3] != cache.D or \
             k.stride(3) != 1 or v.stride(3) != 1:
         raise ValueError("k and v must be [B, rows, heads, D] of the cache's heads and D, of one dtype, with dense heads")
+    _fits(*k.shape)
 
 
 def append_cache(cache, table, lengths, k, v, positions=None, freqs=None, sections=None, interleaved: bool = False,
@@ -922,7 +933,9 @@ def append_cache(cache, table, lengths, k, v, positions=None, freqs=None, sectio
 def attend_trees_workspace_bytes(dtype, B: int, M: int, q_heads: int, cache, width: int) -> int:
     """Bytes of workspace attend_trees needs for trees of M candidates and a table of `width` pages (0: none)."""
     code = {torch.float32: F32, torch.bfloat16: BF16}[dtype]
-    return int(load().lantern_attend_trees_workspace_bytes(code, int(B), int(M), int(q_heads), ctypes.byref(_cache_args(cache)[0]), int(width)))
+    sizes = int(B), int(M), int(q_heads), int(width)
+    _fits(*sizes)
+    return int(load().lantern_attend_trees_workspace_bytes(code, *sizes[:3], ctypes.byref(_cache_args(cache)[0]), sizes[3]))
 
 
 def attend_trees(q, k, v, parent, cache, table, lengths, scale=None, workspace=None, stream=None):
@@ -940,6 +953,7 @@ def attend_trees(q, k, v, parent, cache, table, lengths, scale=None, workspace=N
     B, T = k.shape[:2]
     if q.dim() != 4 or q.shape[:2] != k.shape[:2] or q.shape[3] != c.D or q.dtype != k.dtype or q.stride(3) != 1:
         raise ValueError("q must be [B, rows, heads, D] like k and v, with dense heads")
+    _fits(*q.shape)
     _table_args(table, lengths, B)
     if parent is not None and (parent.dtype != torch.int32 or parent.numel() != B * (T - 1) or not parent.is_contiguous()):
         raise ValueError("parent must be a contiguous int32 tensor of B*M entries")

@@ -395,8 +395,10 @@ bool cache_of(PyObject* o, lantern_cache* c) {
     if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) return false;
     const at::Tensor *k = near(PyTuple_GET_ITEM(o, 0)), *v = near(PyTuple_GET_ITEM(o, 1));
     if (!k || !v || k->dim() != 4 || v->dim() != 4 || !k->is_contiguous() || !v->is_contiguous() || k->scalar_type() != v->scalar_type() ||
-        v->size(0) != k->size(0) || v->size(1) != k->size(1) || v->size(2) != k->size(3) || v->size(3) != k->size(2) || k->size(0) > INT_MAX || recorded(*k) || recorded(*v))
+        v->size(0) != k->size(0) || v->size(1) != k->size(1) || v->size(2) != k->size(3) || v->size(3) != k->size(2) || recorded(*k) || recorded(*v))
         return false;
+    for (int i = 0; i < 4; ++i)
+        if (k->size(i) > INT_MAX) return false;
     *c = {k->data_ptr(), v->data_ptr(), nullptr, nullptr, LANTERN_BF16, (int)k->size(0), (int)k->size(1), (int)k->size(2), (int)k->size(3)};
     if (k->scalar_type() == at::kBFloat16) return true;
     const at::Tensor *ks = near(PyTuple_GET_ITEM(o, 2), at::kFloat), *vs = near(PyTuple_GET_ITEM(o, 3), at::kFloat);

@@ -133,3 +133,36 @@ def test_a_path_without_candidates(lib):
         L.append_cache(**kw)
     assert not lib.called
     L.append_cache(**{**kw, "path": None})
+
+
+def _far(*size, dtype=torch.float32):
+    return torch.empty(size, dtype=dtype, device="meta")
+
+
+FAR = (1 << 32) + 1      # one, when it is cut off to 32 bits
+BEYOND = [("rotate_axes", dict(q=_far(FAR, 1, 32), k=None, positions=_far(FAR, 2, dtype=torch.int32))),
+          ("rotate_axes", dict(q=_far(8, FAR, 32))), ("rotate_axes", dict(k=_far(8, FAR, 32))), ("rotate_axes", dict(q=_far(8, 1, FAR), k=None)),
+          ("rotate_axes", dict(sections=((1 << 32) + 16, -(1 << 32) - 8))),
+          ("append_cache", dict(k=_far(2, FAR, 2, 32), v=_far(2, FAR, 2, 32), positions=None, path=None, count=None)),
+          ("append_cache", dict(table=_far(2, FAR, dtype=torch.int32))),
+          ("append_cache", dict(cache=(_far(FAR, 2, 16, 32, dtype=torch.bfloat16), _far(FAR, 2, 32, 16, dtype=torch.bfloat16), None, None))),
+          ("attend_trees", dict(cache=(_far(9, 2, FAR + 15, 32, dtype=torch.bfloat16), _far(9, 2, 32, FAR + 15, dtype=torch.bfloat16), None, None))),
+          ("attend_trees", dict(q=_far(2, FAR, 4, 32), k=_far(2, FAR, 2, 32), v=_far(2, FAR, 2, 32), parent=None)),
+          ("attend_trees", dict(q=_far(2, 4, FAR + 1, 32))), ("attend_trees", dict(table=_far(2, FAR, dtype=torch.int32)))]
+
+
+@pytest.mark.parametrize("i", range(len(BEYOND)))
+def test_sizes_beyond_32_bits(lib, i):
+    """They would be cut off on their way to the library and serve a part of the call."""
+    name, kw = BEYOND[i]
+    with pytest.raises(ValueError, match="fit 32 bits"):
+        getattr(L, name)(**{**_calls()[name], **kw})
+    assert not lib.called
+
+
+def test_workspace_of_sizes_beyond_32_bits(lib):
+    cache = _calls()["attend_trees"]["cache"]
+    for sizes in ((FAR, 5, 8, 400), (1, FAR, 8, 400), (1, 5, FAR + 7, 400), (1, 5, 8, FAR)):
+        with pytest.raises(ValueError, match="fit 32 bits"):
+            L.attend_trees_workspace_bytes(torch.bfloat16, *sizes[:3], cache, sizes[3])
+    assert not lib.called
