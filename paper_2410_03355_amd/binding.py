@@ -828,6 +828,11 @@ def _nothing_recorded(*tensors):
         raise ValueError("there is no backward pass here: call it under torch.no_grad()")
 
 
+def _written(*tensors):
+    """Tensors of the caller's that a call has written: autograd, which may have saved them, sees a new version."""
+    torch.autograd.graph.increment_version([t for t in tensors if not t.is_inference()])
+
+
 class _Turned(torch.autograd.Function):
     """rotate_axes where gradients are wanted: turning is orthogonal, so theirs is to turn back."""
 
@@ -860,8 +865,9 @@ def rotate_axes(q, k, positions, freqs, sections, interleaved: bool = False, inv
         if t.dim() != 3 or t.shape[0] != q.shape[0] or t.shape[2] != q.shape[2] or t.dtype != q.dtype or (t.shape[2] > 1 and t.stride(2) != 1):
             raise ValueError("q and k must be [N, heads, D] of the same N, D and dtype, with dense heads")
         _fits(*t.shape)
-    _no_tangents(*ts, freqs)
-    if _wants_gradients(*ts, freqs):
+    recorded = (*ts, freqs, *(() if out is None else out))
+    _no_tangents(*recorded)
+    if _wants_gradients(*recorded):
         if out is not None or stream is not None or freqs.requires_grad:
             raise ValueError("gradients are recorded without out and stream, and freqs have none")
         return _Turned.apply(q, k, positions, freqs, sections, interleaved, inverse)
@@ -884,6 +890,8 @@ def rotate_axes(q, k, positions, freqs, sections, interleaved: bool = False, inv
                                  _stream_ptr(stream))
     if rc != OK:
         raise LanternError(rc, "lantern_rotate_axes")
+    if out is not None:
+        _written(*outs)
     return outs[0], outs[1] if has_k else None
 
 
@@ -927,6 +935,7 @@ def append_cache(cache, table, lengths, k, v, positions=None, freqs=None, sectio
                                   None if count is None else count.data_ptr(), out.data_ptr(), _stream_ptr(stream))
     if rc != OK:
         raise LanternError(rc, "lantern_append_cache")
+    _written(*parts)
     return out
 
 

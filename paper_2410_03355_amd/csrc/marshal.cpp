@@ -472,6 +472,10 @@ PyObject* append_cache(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
                               (int)k->size(1), k->const_data_ptr(), k->strides().data(), v->const_data_ptr(), v->strides().data(), type,
                               a[5] == Py_None ? nullptr : &r, path ? path->const_data_ptr<int32_t>() : nullptr,
                               some ? some->const_data_ptr<int32_t>() : nullptr, data(out), current_stream());)
+    for (int p = 0; p < (c.dtype == LANTERN_E4M3 ? 4 : 2) && status == 0; ++p) {      // written: autograd, which may have saved them, sees a new version
+        const at::Tensor& t = THPVariable_Unpack(PyTuple_GET_ITEM(a[0], p));
+        if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+    }
     return single(result(status, out));
 }
 

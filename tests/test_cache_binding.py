@@ -166,3 +166,39 @@ def test_workspace_of_sizes_beyond_32_bits(lib):
         with pytest.raises(ValueError, match="fit 32 bits"):
             L.attend_trees_workspace_bytes(torch.bfloat16, *sizes[:3], cache, sizes[3])
     assert not lib.called
+
+
+def _saved(t):
+    """A result whose backward pass wants `t` as it is."""
+    return (torch.ones((), requires_grad=True) * t).sum()
+
+
+def test_written_tensors_have_a_new_version(lib):
+    """What a call writes in place may have been saved for a backward pass, which has to notice."""
+    kw = _calls()["rotate_axes"]
+    later = [_saved(kw["q"]), _saved(kw["k"])]
+    L.rotate_axes(**kw)
+    assert kw["q"]._version == 0 and kw["positions"]._version == 0
+    L.rotate_axes(**kw, out=(kw["q"], kw["k"]))
+    for y in later:
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+    kw = _calls()["append_cache"]
+    versions = [t._version for t in kw["cache"]]
+    L.append_cache(**kw)
+    assert [t._version for t in kw["cache"]] == [n + 1 for n in versions]
+    with torch.inference_mode():      # tensors without versions
+        kw = _calls()["append_cache"]
+        L.append_cache(**kw)
+        kw = _calls()["rotate_axes"]
+        L.rotate_axes(**kw, out=(kw["q"], kw["k"]))
+
+
+def test_outputs_that_want_gradients(lib):
+    kw = _calls()["rotate_axes"]
+    out = kw["q"].clone().requires_grad_(), kw["k"].clone()
+    with pytest.raises(ValueError, match="gradients are recorded"):
+        L.rotate_axes(**kw, out=out)
+    assert not lib.called
+    with torch.no_grad():
+        L.rotate_axes(**kw, out=out)

@@ -46,3 +46,22 @@ def test_a_cache_that_wants_gradients(lantern_gpu, eight):
                 getattr(lantern_gpu, name)(*args)
             with torch.no_grad():
                 assert torch.equal(getattr(lantern_gpu, name)(*args), want)
+
+
+@pytest.mark.parametrize("eight", [True, False])
+def test_written_tensors_have_a_new_version(lantern_gpu, eight):
+    calls = _calls(lantern_gpu, eight)
+    args, _ = calls["append_cache"]
+    cache = [t for t in args[0] if t is not None]
+    versions = [t._version for t in cache]
+    lantern_gpu.append_cache(*args)
+    assert [t._version for t in cache] == [n + 1 for n in versions]
+    args, _ = calls["rotate_axes"]
+    q, k = args[0].clone(), args[1].clone()
+    later = (torch.ones((), device="cuda", requires_grad=True) * q).sum()
+    lantern_gpu.rotate_axes(q, k, *args[2:], out=(q, k))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        later.backward()
+    with torch.inference_mode():
+        args, _ = _calls(lantern_gpu, eight)["append_cache"]
+        lantern_gpu.append_cache(*args)
