@@ -474,7 +474,7 @@ template <typename T, bool EIGHT>
 static hipError_t launch(const AppendArgs& a, hipStream_t stream) {
     const int units = std::max(rotation_units<4>(a.pairs, a.cache.D), a.cache.D / 8);
     // A wavefront holds 64 units: up to four times that in rows, and the accepted candidates of a tree, which are few
-    if (a.path || a.T * units <= 4 * WAVE) {
+    if (a.path || (int64_t)a.T * units <= 4 * WAVE) {
         const int64_t items = 2 * (int64_t)a.B * a.touched * a.cache.heads;
         if (items > MOST_GROUPS * NW) return hipErrorInvalidConfiguration;
         hipLaunchKernelGGL((append_rows_kernel<T, EIGHT>), dim3((unsigned)((items + NW - 1) / NW)), dim3(NT), 0, stream, a);
