@@ -6,8 +6,9 @@
 // take them: through LDS.
 //
 // Measured: accepted paths of 64 trees, 20 heads of 64, 8 bits 8.7 us, bound by loads one after the other (path, page, row, old scale); 16
-// prompts of about 1000 tokens, 8 heads of 128, 8 bits 39 us, 2.3 TB/s, bound by issue (fp64 angles, rounding, turning over); with one kernel for
-// both 18 and 66.
+// prompts of about 1000 tokens, 8 heads of 128, 8 bits 39 us, 2.3 TB/s; with one kernel for both 18 and 66.  The latter are bound by waiting: wavefronts
+// wait for 54 % of their time, on loads and for each other, and the vector units work 36 % of it, since 174 registers (a thread's rows of a page, keys
+// and values in one kernel) leave two workgroups to a CU.  On pages of 128 tokens (256 and 98 more, one workgroup to a CU) the same takes 80 us.
 //
 // 8-bit pages: value = code * scale.  The scale is the smallest power of two s with largest <= 448 s.  A code has four
 // significant bits under any scale, so nothing is lost against largest / 448 but part of one of e4m3's fifteen binades;
@@ -462,7 +463,8 @@ static hipError_t launch_pages(const AppendArgs& a, hipStream_t stream) {
     const size_t lds = lds_bytes<T>(a.cache);
     const hipError_t e = allow_lds<append_pages_kernel<T, EIGHT, EACH>>(lds);
     if (e != hipSuccess) return e;
-    // Several heads to a workgroup, for whose keys the angles are formed once, while there are four workgroups and more to a CU.
+    // Several heads to a workgroup, for whose keys the angles are formed once, while there are four workgroups and more to a CU (of which the forms
+    // for pages of 64 tokens of 128 and for 128 tokens have two and one resident at once).
     const int64_t places = 2 * (int64_t)a.B * a.touched;
     const int each = (int)std::max<int64_t>(1, std::min<int64_t>(a.cache.heads, places * a.cache.heads / 1024));
     hipLaunchKernelGGL((append_pages_kernel<T, EIGHT, EACH>), dim3(a.B * a.touched, (a.cache.heads + each - 1) / each, 2), dim3(NT), lds, stream, a,

@@ -16,9 +16,13 @@
 // row tiles are too few to fill the device a sequence is split over workgroups as well, whose parts a second kernel joins.
 //
 // Measured (kernel time; 8-bit cache, bf16, unless said): 8 single tokens of 32 heads on 4 of 128 behind 4099 to 32768 tokens 32 us and 5 for the join,
-// 4.7 TB/s, where a large copy reaches 5.1; 64 trees of 61 rows, 20 heads of 64 over 120 to 690 tokens 45.5 us, bound by latency and issue (half of
-// the vector instructions are prologue, own rows and join); 4 trees of 33 rows, 32 heads on 8 of 128 behind 2000 to 16001 tokens 56 + 5 us, 319
-// TFLOP/s, bound by matrix and vector instructions that overlap by a fifth; one token over 577 tokens 9 us, five loads one after the other.
+// 4.7 TB/s, where a large copy reaches 5.1; 64 trees of 61 rows, 20 heads of 64 over 120 to 690 tokens 45.7 us, bound by latency and issue (half of
+// the vector instructions are prologue, own rows and join); 4 trees of 33 rows, 32 heads on 8 of 128 behind 2000 to 16001 tokens 57 + 5 us, 315
+// TFLOP/s: vector units 46 k and matrix units 24 k of 136 k cycles, 1.4 wavefronts to a SIMD on the average, which wait for a third of their
+// time; one token over 577 tokens 9 us, five loads one after the other.
+//
+// Registers.  The bounds at the kernel let two workgroups to a CU (bf16 up to 64 elements: three).  Two instances pay with scratch memory: bf16 over 8
+// bits, D = 128, two tiles of rows 6 registers, and fp32, D = 128, two tiles 39 over 16 bits and 106 over 8 bits (D = 96 over 8 bits: 1).
 #include <hip/hip_runtime.h>
 #include <float.h>
 #include <limits.h>
@@ -195,6 +199,9 @@ struct Rows {
     // Scores of 32 tokens -> weights.  f > 0: the scores' scale in this lane; vs: what the weights are multiplied by for the second product.
     // Tokens that are not seen have a score of -inf.  EARLIER: there are weights that have been summed and wait for the second product.  The
     // maximum is a whole number, upwards: a step of it is a power of two, by which earlier weights, bf16 ones too, are moved exactly.
+    // With bf16 operands a weight is rounded to bf16, which the matrix instructions take, at most half a step of 2^-8 of it, and the sum takes
+    // it as rounded, so what all weights are off by alike cancels.  1.6e-3 of an output (relative, over listed calls) where the output's own rounding
+    // is 1.7e-3, 2.3e-3 together; a second operand for what the rounding leaves would be half as many matrix instructions again.
     template <bool EARLIER>
     __device__ __forceinline__ void weigh(const f32x4 (&s)[QT][2], float f, float vs, Operand (&p)[QT], Operand (&earlier)[QT]) {
         float top[QT];
@@ -907,12 +914,15 @@ __global__ __launch_bounds__(NT) void attend_join_kernel(AttendArgs a) {
 AttendPlan plan_attend(int dtype, int B, int M, int q_heads, const lantern_cache& c, int width) {
     AttendPlan p;
     const int64_t R = (int64_t)(M + 1) * (q_heads / c.heads);
-    const int64_t room = dtype == LANTERN_BF16 && c.D <= 64 ? 768 : 512;      // workgroups that fit the 256 CUs at once
+    // Workgroups that are counted on to be resident on the 256 CUs: what the kernel's bound on registers lets in.  That is what fits with two tiles of
+    // rows from D = 64 on, but for fp32 over 8 bits with D = 96 and 128, whose 82 and 108 KiB of LDS leave one to a CU, and D = 128 with trees of
+    // about 160 rows and more over 8 bits (fp32: over 16).  With D = 32, and with one tile at D = 64 (bf16, and fp32 over 16 bits), four and more fit.
+    const int64_t room = dtype == LANTERN_BF16 && c.D <= 64 ? 768 : 512;
     const int64_t tokens = (int64_t)width * c.page_tokens, tile = c.dtype == LANTERN_E4M3 ? 64 : 32;
     const int64_t useful = std::max<int64_t>(1, tokens / (tile * NW * 2));    // parts of two tiles to a wavefront at least
     // Tiles of 16 rows that a wavefront takes together: each conversion of a tile of tokens serves all of them.  Four (D <= 64, 246 registers)
     // were no faster where they had all their use: 64 trees of 61 rows 55.1 us against 53.8 with two, one tree 14.8 against 11.3.  One, where
-    // all workgroups fit at once and sequences are not cut: a wavefront has less to do (one tree of 61 rows behind 640 tokens 9.9 us against 11.0, 8
+    // all workgroups are counted to fit at once and sequences are not cut: a wavefront has less to do (one tree of 61 rows behind 640 tokens 9.9 us against 11.0, 8
     // of 33 11.6 against 13.1, but 26 of 33 23.4 against 21.7, and long sequences behind 33 rows 32 against 27).  Also in fp32, bound by its
     // products, where one leaves a sixth less of empty rows (20 trees of 33 rows 50 us against 61, of 66 97 against 102, but 132 rows 191
     // against 192 and less with shorter heads).

@@ -39,7 +39,7 @@ struct AppendArgs {
     int32_t* out_lengths;
 };
 
-// Division by a number that the host knows, for 0 <= n < 2^31.  With 2^(l-1) < d <= 2^l and mul = floor(2^32 (2^l - d) / d) + 1 the
+// Division by a number that the host knows, for 0 <= n < 2^31 (Granlund and Montgomery 1994, division by invariant integers).  With 2^(l-1) < d <= 2^l and mul = floor(2^32 (2^l - d) / d) + 1 the
 // quotient is (umulhi(n, mul) + n) >> l.
 struct Divisor {
     unsigned mul;
