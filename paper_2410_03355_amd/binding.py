@@ -205,19 +205,20 @@ def _stream_ptr(stream) -> int:
     return int(s.cuda_stream)
 
 
-def _room(stream, size, dtype, device):
-    """Memory for work on `stream` (None: the current one), from that stream's own: what the current stream has freed may still be read or
-    written by work queued there, which another stream does not wait for."""
-    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-        return torch.empty(size, dtype=dtype, device=device)
-
-
-def _output(stream, size, dtype, device):
-    """The same for what the caller gets: once dropped it is given away when the current stream, which may read it, has come to that place."""
-    t = _room(stream, size, dtype, device)
-    if stream is not None:
-        t.record_stream(torch.cuda.current_stream(t.device))
-    return t
+def _outputs(stream, device, *sizes, dtype=torch.int32, workspace: int = 0):
+    """Tensors for the results of work on `stream` (None: the current one), and behind them one of `workspace` bytes if that is not 0.  Their memory
+    is that stream's own: what the current stream has freed may still be read or written by work queued there, which another stream does not
+    wait for.  And results, once dropped, are given away when the current stream, which may read them, has come to that place."""
+    if not (sizes or workspace):
+        return []
+    current = None if stream is None else torch.cuda.current_stream(device)
+    with contextlib.nullcontext() if current == stream else torch.cuda.stream(stream):
+        made = [torch.empty(size, dtype=dtype, device=device) for size in sizes]
+        room = [torch.empty(workspace, dtype=torch.uint8, device=device)] if workspace else []
+    if current != stream:
+        for t in made:
+            t.record_stream(current)
+    return made + room
 
 
 def _need_cuda(*tensors):
@@ -246,14 +247,14 @@ def build_knn(codebook: torch.Tensor, k: int, metric: str = "l2", stream=None, r
     if nbytes == 0:
         raise LanternError(E_SHAPE, "lantern_build_knn_workspace_bytes")
     if workspace is None:
-        ws = (_output if return_stats else _room)(stream, nbytes, torch.uint8, codebook.device)
+        (ws,) = _outputs(stream, codebook.device, nbytes, dtype=torch.uint8) if return_stats else _outputs(stream, codebook.device, workspace=nbytes)
     else:
         _need_cuda(workspace)
         if workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.numel() < nbytes:
             raise ValueError("workspace must be a contiguous uint8 tensor of at least knn_workspace_bytes")
         ws = workspace
     if out is None:
-        out = _output(stream, (V, k), torch.int32, codebook.device)
+        (out,) = _outputs(stream, codebook.device, (V, k))
     else:
         _need_cuda(out)
         if out.dtype != torch.int32 or tuple(out.shape) != (V, k) or not out.is_contiguous():
@@ -334,8 +335,9 @@ def verify(target_logits, draft_logits, draft_tokens, knn, delta: float, uniform
             return got
     N, V, k = _check_verify_args(target_logits, draft_logits, draft_tokens, knn, uniforms)
     dev = target_logits.device
-    acc = _output(stream, N, torch.int32, dev) if out_accept is None else out_accept
-    res = _output(stream, N, torch.int32, dev) if out_resample is None else out_resample
+    made = _outputs(stream, dev, *[N for t in (out_accept, out_resample) if t is None])
+    acc = made[0] if out_accept is None else out_accept
+    res = made[-1] if out_resample is None else out_resample
     rc = lib.lantern_verify(target_logits.data_ptr(), draft_logits.data_ptr(),
                             _dtype_code(target_logits), N, V, target_logits.stride(0) if N > 1 else V,
                             draft_tokens.data_ptr(), knn.data_ptr(), k, float(delta),
@@ -357,15 +359,9 @@ def verify_ex(target_logits, draft_logits, draft_tokens, knn, delta: float, unif
     lib = load()
     N, V, k = _check_verify_args(target_logits, draft_logits, draft_tokens, knn, uniforms)
     dev = target_logits.device
-    out = {
-        "accept": _output(stream, N, torch.int32, dev),
-        "resample": _output(stream, N, torch.int32, dev),
-        "accept_prob": _output(stream, N, torch.float32, dev),
-        "mass": _output(stream, N, torch.float32, dev),
-        "g_tok": _output(stream, N, torch.float32, dev),
-        "a_size": _output(stream, N, torch.int32, dev),
-        "path": _output(stream, N, torch.int32, dev),
-    }
+    acc, res, size, path = _outputs(stream, dev, N, N, N, N)
+    prob, mass, g_tok = _outputs(stream, dev, N, N, N, dtype=torch.float32)
+    out = {"accept": acc, "resample": res, "accept_prob": prob, "mass": mass, "g_tok": g_tok, "a_size": size, "path": path}
     common_in = (target_logits.data_ptr(), draft_logits.data_ptr(), _dtype_code(target_logits), N, V,
                  target_logits.stride(0) if N > 1 else V, draft_tokens.data_ptr(), knn.data_ptr(), k)
     common_out = (uniforms.data_ptr(), out["accept"].data_ptr(), out["resample"].data_ptr(),
@@ -399,9 +395,8 @@ def verify_greedy(target_logits, draft_tokens, knn, delta: float, stream=None, w
     if not (draft_tokens.is_contiguous() and knn.is_contiguous()):
         raise ValueError("draft_tokens and knn must be contiguous")
     dev = target_logits.device
-    acc = _output(stream, N, torch.int32, dev)
-    tok = _output(stream, N, torch.int32, dev)
-    path = _output(stream, N, torch.int32, dev) if want_path else None
+    acc, tok, *path = _outputs(stream, dev, *[N] * (3 if want_path else 2))
+    path = path[0] if want_path else None
     rc = lib.lantern_verify_greedy(target_logits.data_ptr(), _dtype_code(target_logits), N, V,
                                    target_logits.stride(0) if N > 1 else V, draft_tokens.data_ptr(),
                                    knn.data_ptr(), int(knn.shape[1]), float(delta), acc.data_ptr(),
@@ -428,8 +423,7 @@ def accept_chains(accept, resample, L: int, stream=None):
     if not (accept.is_contiguous() and resample.is_contiguous()):
         raise ValueError("accept and resample must be contiguous")
     B = accept.numel() // L
-    kept = _output(stream, B, torch.int32, accept.device)
-    nxt = _output(stream, B, torch.int32, accept.device)
+    kept, nxt = _outputs(stream, accept.device, B, B)
     rc = lib.lantern_accept_chains(accept.data_ptr(), resample.data_ptr(), B, int(L), kept.data_ptr(),
                                    nxt.data_ptr(), _stream_ptr(stream))
     if rc != OK:
@@ -468,8 +462,7 @@ def verify_rows(target_logits, draft_logits, row_index, draft_tokens, knn, delta
     if not (draft_tokens.is_contiguous() and knn.is_contiguous() and uniforms.is_contiguous()):
         raise ValueError("draft_tokens, knn and uniforms must be contiguous")
     dev = target_logits.device
-    acc = _output(stream, N, torch.int32, dev)
-    res = _output(stream, N, torch.int32, dev)
+    acc, res = _outputs(stream, dev, N, N)
     rc = lib.lantern_verify_rows(target_logits.data_ptr(), draft_logits.data_ptr(), _dtype_code(target_logits),
                                  R, V, target_logits.stride(0) if R > 1 else V, row_index.data_ptr(), N,
                                  draft_tokens.data_ptr(), knn.data_ptr(), int(knn.shape[1]),
@@ -498,8 +491,7 @@ def verify_greedy_rows(target_logits, row_index, draft_tokens, knn, delta: float
     if knn.dim() != 2 or knn.shape[0] != V or not (draft_tokens.is_contiguous() and knn.is_contiguous()):
         raise ValueError("the table must be a contiguous [V, k] tensor, the tokens contiguous")
     dev = target_logits.device
-    acc = _output(stream, N, torch.int32, dev)
-    tok = _output(stream, N, torch.int32, dev)
+    acc, tok = _outputs(stream, dev, N, N)
     rc = lib.lantern_verify_greedy_rows(target_logits.data_ptr(), _dtype_code(target_logits), R, V,
                                         target_logits.stride(0) if R > 1 else V, row_index.data_ptr(), N,
                                         draft_tokens.data_ptr(), knn.data_ptr(), int(knn.shape[1]), float(delta),
@@ -526,9 +518,7 @@ def accept_trees(accept, resample, parent, M: int, stream=None):
         raise ValueError("accept, resample and parent must hold B*M rows")
     B = accept.numel() // M
     dev = accept.device
-    n = _output(stream, B, torch.int32, dev)
-    path = _output(stream, (B, M), torch.int32, dev)
-    nxt = _output(stream, B, torch.int32, dev)
+    n, path, nxt = _outputs(stream, dev, B, (B, M), B)
     rc = lib.lantern_accept_trees(accept.data_ptr(), None if resample is None else resample.data_ptr(),
                                   parent.data_ptr(), B, int(M),
                                   n.data_ptr(), path.data_ptr(), nxt.data_ptr(), _stream_ptr(stream))
@@ -543,7 +533,7 @@ RANDOM_MAX_K = 4096
 def build_random(V: int, k: int, seed: int, device="cuda", stream=None):
     """lantern_build_random; returns the [V, k] int32 table on the device."""
     lib = load()
-    out = _output(stream, (V, k), torch.int32, device)
+    (out,) = _outputs(stream, device, (V, k))
     rc = lib.lantern_build_random(int(V), int(k), int(seed) & 0xFFFFFFFFFFFFFFFF, out.data_ptr(),
                                   _stream_ptr(stream))
     if rc != OK:
@@ -584,8 +574,8 @@ def decide_rows(target_logits, draft_logits, row_index, draft_tokens, knn, delta
         if got is not None:
             return _checked_status(got, "lantern_decide_rows")
     R, V, N, stride = _rows_args(target_logits, draft_logits, row_index, draft_tokens, knn, uniforms)
-    acc = _output(stream, N, torch.int32, target_logits.device)
-    path = _output(stream, N, torch.int32, target_logits.device) if want_path else None
+    acc, *path = _outputs(stream, target_logits.device, *[N] * (2 if want_path else 1))
+    path = path[0] if want_path else None
     rc = lib.lantern_decide_rows(target_logits.data_ptr(), draft_logits.data_ptr(), _dtype_code(target_logits),
                                  R, V, stride, None if row_index is None else row_index.data_ptr(), N,
                                  draft_tokens.data_ptr(), knn.data_ptr(), int(knn.shape[1]),
@@ -605,7 +595,7 @@ def resample_selected(target_logits, draft_logits, row_index, draft_tokens, knn,
     _need_cuda(select)
     if select.dtype != torch.int32 or not select.is_contiguous():
         raise TypeError("select must be a contiguous int32 tensor")
-    out = _output(stream, select.numel(), torch.int32, target_logits.device)
+    (out,) = _outputs(stream, target_logits.device, select.numel())
     rc = lib.lantern_resample_selected(target_logits.data_ptr(), draft_logits.data_ptr(),
                                        _dtype_code(target_logits), R, V, stride,
                                        None if row_index is None else row_index.data_ptr(), N,
@@ -632,10 +622,7 @@ def verify_trees(target_logits, draft_logits, row_index, parent, M: int, draft_t
         raise ValueError("parent must be a contiguous int32 tensor of B*M entries")
     B = N // M
     dev = target_logits.device
-    acc = _output(stream, N, torch.int32, dev)
-    n = _output(stream, B, torch.int32, dev)
-    path = _output(stream, (B, M), torch.int32, dev)
-    nxt = _output(stream, B, torch.int32, dev)
+    acc, n, path, nxt = _outputs(stream, dev, N, B, (B, M), B)
     rc = lib.lantern_verify_trees(target_logits.data_ptr(), draft_logits.data_ptr(), _dtype_code(target_logits),
                                   R, V, stride, None if row_index is None else row_index.data_ptr(),
                                   parent.data_ptr(), B, int(M),
@@ -665,12 +652,9 @@ def verify_trees_sequential(target_logits, draft_logits, row_index, parent, M: i
     B = N // M
     dev = target_logits.device
     need = int(lib.lantern_verify_trees_sequential_workspace_bytes(B, int(M), V))
-    if workspace is None:
-        workspace = _room(stream, max(need, 256), torch.uint8, dev)
     _need_cuda(workspace)
-    n = _output(stream, B, torch.int32, dev)
-    path = _output(stream, (B, M), torch.int32, dev)
-    nxt = _output(stream, B, torch.int32, dev)
+    n, path, nxt, *room = _outputs(stream, dev, B, (B, M), B, workspace=max(need, 256) if workspace is None else 0)
+    workspace = room[0] if room else workspace
     rc = lib.lantern_verify_trees_sequential(target_logits.data_ptr(), draft_logits.data_ptr(),
                                              _dtype_code(target_logits), R, V, stride,
                                              None if row_index is None else row_index.data_ptr(),
@@ -713,11 +697,7 @@ def verify_trees_greedy(target_logits, row_index, parent, M: int, draft_tokens, 
         raise ValueError("shape mismatch between parent, tokens and the table")
     B = N // M
     dev = target_logits.device
-    acc = _output(stream, N, torch.int32, dev)
-    tok = _output(stream, N, torch.int32, dev)
-    n = _output(stream, B, torch.int32, dev)
-    path = _output(stream, (B, M), torch.int32, dev)
-    nxt = _output(stream, B, torch.int32, dev)
+    acc, tok, n, path, nxt = _outputs(stream, dev, N, N, B, (B, M), B)
     rc = lib.lantern_verify_trees_greedy(target_logits.data_ptr(), _dtype_code(target_logits), R, V,
                                          target_logits.stride(0) if R > 1 else V,
                                          None if row_index is None else row_index.data_ptr(), parent.data_ptr(), B,
@@ -876,7 +856,7 @@ def rotate_axes(q, k, positions, freqs, sections, interleaved: bool = False, inv
     code = _dtype_code(q)
     rot = _rotation_args(positions, freqs, sections, interleaved, N)
     if out is None:
-        outs = [_output(stream, t.shape, t.dtype, t.device) for t in ts]
+        outs = _outputs(stream, q.device, *[t.shape for t in ts], dtype=q.dtype)
     else:
         outs = [t for t in out if t is not None]
         if len(outs) != len(ts) or any(o.shape != t.shape or o.dtype != t.dtype or (D > 1 and o.stride(2) != 1) for o, t in zip(outs, ts)):
@@ -928,7 +908,7 @@ def append_cache(cache, table, lengths, k, v, positions=None, freqs=None, sectio
     if path is not None and (count is None or T < 2):
         raise ValueError("path comes with count, and with rows for its candidates")
     _need_here(stream, *parts, table, lengths, k, v, positions, freqs, path, count)
-    out = _output(stream, B, torch.int32, k.device)
+    (out,) = _outputs(stream, k.device, B)
     rc = lib.lantern_append_cache(ctypes.byref(c), table.data_ptr(), table.shape[1], lengths.data_ptr(), B, T, k.data_ptr(),
                                   _strides(*k.stride()[:3]), v.data_ptr(), _strides(*v.stride()[:3]), _dtype_code(k),
                                   None if rot is None else ctypes.byref(rot), None if path is None else path.data_ptr(),
@@ -971,9 +951,8 @@ def attend_trees(q, k, v, parent, cache, table, lengths, scale=None, workspace=N
     _need_here(stream, *parts, table, lengths, q, k, v, parent, workspace)
     code, Hq, width = _dtype_code(q), q.shape[2], table.shape[1]
     need = int(lib.lantern_attend_trees_workspace_bytes(code, B, T - 1, Hq, ctypes.byref(c), width))
-    if workspace is None and need:
-        workspace = _room(stream, need, torch.uint8, q.device)
-    out = _output(stream, (B, T, Hq, c.D), q.dtype, q.device)
+    out, *room = _outputs(stream, q.device, (B, T, Hq, c.D), dtype=q.dtype, workspace=need if workspace is None else 0)
+    workspace = room[0] if room else workspace
     rc = lib.lantern_attend_trees(q.data_ptr(), _strides(*q.stride()[:3]), k.data_ptr(), _strides(*k.stride()[:3]), v.data_ptr(),
                                   _strides(*v.stride()[:3]), code, B, T - 1, Hq, None if parent is None else parent.data_ptr(),
                                   ctypes.byref(c), table.data_ptr(), width, lengths.data_ptr(),

@@ -77,9 +77,30 @@ def test_memory_of_another_stream(watched, name):
     wait for.  Outputs are kept until the current stream has passed the place where they are dropped."""
     side, made, kept = watched
     outs = _tensors(CALLS[name](side))
-    assert len(made) == len(outs) + (name in ("verify_trees_sequential", "build_knn")) and all(inside == 1 for _, inside in made)
+    assert len(made) == len(outs) + (name in ("verify_trees_sequential", "build_knn")) and all(inside for _, inside in made)
     assert sorted(kept) == sorted((o.data_ptr(), "current") for o in outs)
     made.clear()
     kept.clear()
     CALLS[name](None)
     assert made and all(inside == 0 for _, inside in made) and not kept
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_the_current_stream_by_name(watched, name):
+    """Given the current stream itself a call allocates as it does without one."""
+    _, made, kept = watched
+    CALLS[name]("current")
+    assert made and not any(inside for _, inside in made) and not kept
+
+
+def test_nothing_to_allocate(watched, monkeypatch):
+    """With the caller's outputs the streams are not looked at: such calls are captured and timed."""
+    side, made, kept = watched
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: pytest.fail("looked at"))
+    L.verify(t, g, tok, table, 0.1, un, out_accept=acc, out_resample=acc, stream=side)
+    assert not made and not kept
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: "current")
+    got = L.verify(t, g, tok, table, 0.1, un, out_resample=acc, stream=side)
+    assert len(made) == 1 and made[0][1] and got[1] is acc and got[0].data_ptr() == made[0][0]
+    got = L.verify(t, g, tok, table, 0.1, un, out_accept=acc, stream=side)
+    assert got[0] is acc and got[1].data_ptr() == made[1][0]

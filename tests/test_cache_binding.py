@@ -76,7 +76,7 @@ def test_memory_of_another_stream(lib, monkeypatch, name):
     lib.workspace = 4096
     got = getattr(L, name)(**kw, stream=side)
     outs = got if isinstance(got, tuple) else (got,)
-    assert len(made) == len(outs) + (name == "attend_trees") and all(inside == 1 for _, inside in made)
+    assert len(made) == len(outs) + (name == "attend_trees") and all(inside for _, inside in made)
     assert all((o.data_ptr(), "current") in kept for o in outs)
     made.clear()
     kept.clear()
